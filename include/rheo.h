@@ -70,7 +70,8 @@ enum {
     RHEO_ESTATE = -4    /* call out of the step order                    */
 };
 
-enum { RHEO_F32 = 0, RHEO_BF16 = 1 };
+enum { RHEO_F32 = 0, RHEO_BF16 = 1,
+       RHEO_F16 = 2 };  /* rheo_cache_create and rheo_scorer_create alone */
 
 enum { RHEO_METHOD_RHEO = 0, RHEO_METHOD_RRSW = 1, RHEO_METHOD_TOPK = 2 };
 
@@ -265,6 +266,203 @@ int rheo_device_error(rheo_tree* tree, int32_t* host_flag);
 
 /* Nodes per sequence of the unpruned tree (root included). */
 int32_t rheo_node_count(const rheo_tree* tree);
+
+/* ---------------------------------------------------------------------------
+ * The key/value cache around a drafted tree
+ *
+ * The target forward that scores a pruned tree attends from every pruned node
+ * to the tokens before the tree (the prefix) and to the node's ancestors
+ * (rheo_tree_mask).  Keys and values lie in pages:
+ *   k_cache, v_cache  [layers][pages][page_size][kv_heads][head_dim]
+ * of cfg.dtype, page_stride elements between pages and layer_stride between
+ * layers.  A slot is page * page_size + place in the page.  Sequence b holds
+ * held[b] pages, named in order by its row of the block table
+ *   table             [B][table_width] int32
+ * and entry e of the sequence lies in slot
+ * table[b][e / page_size] * page_size + e % page_size.  lens[b] entries are
+ * the prefix; the rows of one step (the pruned tree, root first, or any
+ * other rows) are the entries lens[b] + i behind it.  One step is
+ *     rheo_cache_plan        pages and slots for the rows of the step
+ *     per layer: rheo_cache_write, rheo_tree_attention
+ *     (rheo_verify)
+ *     rheo_cache_commit      the accepted path moved together, lens advanced
+ *     rheo_token_logprobs    (of what was emitted, where asked for)
+ * The caller owns the pages, tables and lengths; the handle owns workspace
+ * and an error flag.  The conventions above hold: device pointers,
+ * work enqueued on `stream` (of the handle's device, whichever is current),
+ * no synchronisation, nothing allocated after creation (so every call may be
+ * captured into a graph), one handle on one stream at a time (two graphs that
+ * share a handle must not run at once).  Strides are in elements; tensor
+ * pointers and strides are multiples of 16 bytes unless noted.
+ * Lengths, tables, slots and tokens are data that the host cannot check: a
+ * value out of range sets a bit of the error flag (rheo_cache_error) and
+ * never reads or writes outside the arrays as declared by the arguments.
+ * ------------------------------------------------------------------------ */
+
+typedef struct rheo_cache rheo_cache;
+
+typedef struct rheo_cache_config {
+    int32_t batch;               /* B, 1..4096 sequences                              */
+    int32_t heads;               /* query heads, a multiple of kv_heads, <= 1024         */
+    int32_t kv_heads;            /* key/value heads, >= 1                               */
+    int32_t head_dim;            /* a multiple of 8, 8..256                             */
+    int32_t page_size;           /* entries of a page: a power of two, 1..4096           */
+    int32_t pages;               /* pages of the pool, >= 1                             */
+    int32_t table_width;         /* pages a sequence may hold, >= 1; table_width *
+                                    page_size < 2^31                                  */
+    int32_t layers;              /* layers one rheo_cache_commit moves, 1..1024          */
+    int32_t dtype;               /* RHEO_BF16 or RHEO_F16                               */
+    int64_t page_stride;         /* >= page_size * kv_heads * head_dim; 0: equal to it   */
+    int64_t layer_stride;        /* >= pages * page_stride; 0: equal to it               */
+} rheo_cache_config;
+
+/* Allocates the workspace (of the current device, which becomes the handle's). */
+int rheo_cache_create(const rheo_cache_config* cfg, rheo_cache** out);
+/* Frees it (synchronises the device). */
+int rheo_cache_destroy(rheo_cache* cache);
+
+/* Synchronises the handle's device and reads its sticky error flag: bit 0:
+ * lens, count, held, free_count or the free list out of range in
+ * rheo_cache_plan; bit 1: a slot >= pages * page_size; bit 2: a position
+ * outside the rotation table; bit 3: a page outside the pool; bit 4: an
+ * accepted token that is no child of the node before it; bit 5: entries
+ * past the table's row. */
+int rheo_cache_error(rheo_cache* cache, int32_t* host_flag);
+
+/* Pages and slots for the next rows of every sequence.
+ * Sequence b needs ceil((lens[b] + count[b]) / page_size) pages (count NULL:
+ * n rows each).  Pages it holds beyond that go back to the free list, pages it
+ * lacks come from it; so a call with n = 0 after a step returns what the
+ * step no longer needs, and with lens[b] = 0 all of a finished sequence.
+ *   lens, count  [B] int32 in; 0 <= count[b] <= n
+ *   depth        [B][n] int32 in, or NULL: i for row i
+ *   held         [B] int32 in/out
+ *   table        [B][table_width] int32 in/out; places at and past held[b]
+ *                are not read, and not written but by a page that comes
+ *   free_list    [pages] int32 in/out, a stack, its top at free_count - 1
+ *   free_count   [1] int32 in/out
+ *   slots        [B][n] int64 out: of entry lens[b] + i, -1 for i >= count[b]
+ *   positions    [B][n] int32 out: lens[b] + depth[b][i], -1 for i >= count[b]
+ *   status       [B] int32 out: 0 served; 1 the free pages do not reach; 2 the
+ *                sequence would not fit its row of the table (or bit 0 above).
+ *                With 1 or 2 the sequence keeps what it has and its slots and
+ *                positions are -1.
+ * Order: returned pages are pushed first, the last page of the last sequence
+ * before all others; then pages are popped for one sequence after another.
+ * A sequence is served iff it lacks none, or the pages lacked by it and by
+ * those before it (served or not) are there.  n = 0: slots, positions and
+ * depth may be NULL. */
+int rheo_cache_plan(rheo_cache* cache, int32_t n, const int32_t* lens, const int32_t* count,
+                    const int32_t* depth, int32_t* held, int32_t* table, int32_t* free_list,
+                    int32_t* free_count, int64_t* slots, int32_t* positions, int32_t* status,
+                    void* stream);
+
+typedef struct rheo_write_args {
+    int32_t n;                   /* rows of a sequence; row (b, i) is row b * n + i       */
+    int32_t rot_dim;             /* leading elements of a head that are rotated, even,
+                                    0..head_dim                                       */
+    int32_t max_position;        /* rows of `rotation`                                  */
+    int32_t interleaved;         /* pairs (2j, 2j+1) instead of (j, j + rot_dim / 2)     */
+    const void* q;               /* [B * n] rows of [heads][head_dim]; or NULL: keys and
+                                    values alone                                      */
+    const void* k;               /* [B * n] rows of [kv_heads][head_dim]                */
+    const void* v;
+    void* q_out;                 /* as q; may be q itself with q's stride               */
+    int64_t q_stride, k_stride, v_stride, q_out_stride;   /* between rows               */
+    const int64_t* slots;        /* [B * n]; a row of slot < 0 is left out whole         */
+    const int32_t* positions;    /* [B * n] int32, or NULL with rot_dim 0               */
+    const float* rotation;       /* [max_position][rot_dim]: cosines, then sines         */
+    const void* q_weight;        /* [head_dim] of cfg.dtype, or NULL: no norm            */
+    const void* k_weight;
+    float eps;                   /* of the norms, >= 0                                  */
+    void* k_cache;               /* one layer's pages                                  */
+    void* v_cache;
+} rheo_write_args;
+
+/* Norm, rotation and store in one pass: each head of q and k is divided by the
+ * root of its mean square plus eps and multiplied by its weight, its first
+ * rot_dim elements are rotated by the row of `rotation` at the row's
+ * position ((a, b) -> (a cos - b sin, b cos + a sin)); q goes to q_out, k
+ * and v to the row's slot.  fp32 inside, one rounding at the end.  Slots of one
+ * call are distinct (else which row stays is undefined); q, k and v do not
+ * overlap the pages. */
+int rheo_cache_write(rheo_cache* cache, const rheo_write_args* args, void* stream);
+
+typedef struct rheo_attention_args {
+    int32_t n;                   /* query rows of a sequence; row (b, i) is row b * n + i */
+    int32_t tail;                /* entries behind the prefix, >= n or with a mask any   */
+    const void* q;               /* [B * n] rows of [heads][head_dim]                   */
+    int64_t q_stride, out_stride;/* between rows                                        */
+    const void* k_cache;         /* one layer's pages                                  */
+    const void* v_cache;
+    const int32_t* table;        /* [B][table_width]                                    */
+    const int32_t* lens;         /* [B] entries of the prefix                            */
+    const int32_t* count;        /* [B] or NULL: the first count[b] of the n rows are
+                                    there and the first tail - (n - count[b]) entries
+                                    behind the prefix                                 */
+    const uint8_t* mask;         /* [B][n][tail], row i attends entry lens[b] + j iff
+                                    not 0; NULL: iff j <= i + tail - n                  */
+    float scale;                 /* > 0                                                 */
+    void* out;                   /* as q; not q itself                                  */
+    float* lse;                  /* [B * n][heads] or NULL: log of the sum of
+                                    exp(scale q.k) over what the row attends            */
+} rheo_attention_args;
+
+/* Attention of the step's rows over the pages: softmax(scale q.k) v over the
+ * whole prefix and the entries behind it that the mask names.  Query head h
+ * reads key/value head h / (heads / kv_heads).  fp32 scores, sums and
+ * accumulators; the probabilities enter the second product in cfg.dtype.  A row
+ * that attends nothing gives 0 and lse -inf.  Rows i >= count[b] are left as
+ * they were.  What a row does not attend has no effect on it, whatever it
+ * holds. */
+int rheo_tree_attention(rheo_cache* cache, const rheo_attention_args* args, void* stream);
+
+/* Keeps the accepted path of a verified tree: with parent and token [B][n] as
+ * rheo_pruned_view gives them (n = R + 1) and accepted [B][depth] and
+ * accept_len [B] as rheo_verify does, the entries of the root and of the
+ * accepted nodes are moved in every layer, keys and values, from lens[b] +
+ * pruned index to lens[b] + 0, 1, 2, ...; the entries between are then free.
+ *   path      [B][depth + 1] int32 out: pruned indices of the root and the
+ *             accepted nodes, -1 past the end (what rheo_token_logprobs takes)
+ *   new_lens  [B] int32 out: lens[b] + 1 + accept_len[b]; may be lens itself
+ * A sequence with accept_len < 0 (a failed walk), or one that sets an error
+ * bit, keeps its entries and length; its path is all -1. */
+int rheo_cache_commit(rheo_cache* cache, int32_t n, int32_t depth, const int32_t* parent,
+                      const int32_t* token, const int32_t* accepted, const int32_t* accept_len,
+                      const int32_t* lens, const int32_t* table, void* k_cache, void* v_cache,
+                      int32_t* path, int32_t* new_lens, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Log probabilities of given tokens
+ * ------------------------------------------------------------------------ */
+
+typedef struct rheo_scorer rheo_scorer;
+
+/* A scorer of logit rows of `vocab` elements (2 <= vocab <= 2^24), row_stride
+ * elements apart (conventions as for logit rows above; RHEO_F32, RHEO_BF16 or
+ * RHEO_F16).  It owns a workspace of fixed size. */
+int rheo_scorer_create(int32_t vocab, int32_t dtype, int64_t row_stride, rheo_scorer** out);
+int rheo_scorer_destroy(rheo_scorer* scorer);
+
+/* For the token of every entry (b, j), p = softmax(row / T):
+ *   logits       [B][n][row_stride]
+ *   path         [B][m] int32: the entry's row of the sequence's n, or NULL: row j
+ *                (m <= n)
+ *   token        [B][m] int32
+ *   logprob      [B][m] float out: ln p of the token
+ *   entropy      [B][m] float out: -sum p ln p
+ *   rank         [B][m] int32 out: tokens that precede it by (logit descending,
+ *                id ascending)
+ *   top_token    [B][m][top] int32 out, top_logprob [B][m][top] float out: the
+ *                first `top` tokens of that order, 0 <= top <= 32 and <= vocab
+ * entropy, rank and, with top = 0, the last two may be NULL.  Entries whose
+ * path lies outside [0, n) or whose token lies outside [0, vocab) are left as
+ * they were.  -inf is a token of probability 0; a row without a finite logit
+ * has no distribution: NaN. */
+int rheo_token_logprobs(rheo_scorer* scorer, const void* logits, int32_t B, int32_t n,
+                        const int32_t* path, const int32_t* token, int32_t m, int32_t top,
+                        float T, float* logprob, float* entropy, int32_t* rank,
+                        int32_t* top_token, float* top_logprob, void* stream);
 
 /* Message of the calling thread's last failed call ("" if none). */
 const char* rheo_last_error(void);

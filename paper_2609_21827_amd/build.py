@@ -8,22 +8,26 @@ fp32 instructions.
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librheo.so")
 PROBE_LIB = os.path.join(HERE, "libstreamprobe.so")
-SOURCES = ["api.hip", "expand.hip", "dense.hip", "prune.hip", "verify.hip", "views.hip"]
+SOURCES = ["api.hip", "expand.hip", "dense.hip", "prune.hip", "verify.hip", "views.hip",
+           "cache_api.hip", "cache_plan.hip", "cache_write.hip", "attention.hip",
+           "cache_commit.hip", "logprobs.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 
-def _compile(out, sources, verbose):
-    cmd = [HIPCC, "-O3", "--offload-arch=gfx950", "-std=c++17", "-shared", "-fPIC",
-           "-ffp-contract=off", "-fno-fast-math",
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-           "-o", out + ".tmp"] + [os.path.join(CSRC, s) for s in sources]
+FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC",
+         "-ffp-contract=off", "-fno-fast-math",
+         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+         "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+
+
+def _run(cmd, verbose):
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -32,15 +36,26 @@ def _compile(out, sources, verbose):
     if res.returncode != 0:
         raise RuntimeError("hipcc failed:\n" + "\n".join(msgs))
     if verbose and msgs:
-        print("\n".join(msgs))
+        print("\n".join(msgs), flush=True)
+
+
+def _compile(out, sources, verbose, jobs=None):
+    """One object per source, `jobs` compilers at a time, then the library."""
+    objs = [os.path.join(HERE, "build", os.path.basename(out) + "." + s + ".o") for s in sources]
+    os.makedirs(os.path.join(HERE, "build"), exist_ok=True)
+    with ThreadPoolExecutor(jobs or min(4, os.cpu_count() or 1)) as pool:
+        list(pool.map(lambda so: _run([HIPCC] + FLAGS + ["-c", os.path.join(CSRC, so[0]),
+                                                         "-o", so[1]], verbose),
+                      zip(sources, objs)))
+    _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", out + ".tmp"] + objs, verbose)
     os.replace(out + ".tmp", out)
     return out
 
 
 def build(verbose=False, jobs=None):
     """librheo.so, and the streaming-read probe bench.py measures beside it."""
-    _compile(PROBE_LIB, ["stream_probe.hip"], verbose)
-    return _compile(LIB, SOURCES, verbose)
+    _compile(PROBE_LIB, ["stream_probe.hip"], verbose, jobs)
+    return _compile(LIB, SOURCES, verbose, jobs)
 
 
 if __name__ == "__main__":

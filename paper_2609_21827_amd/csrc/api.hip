@@ -10,6 +10,7 @@
 
 #include <mutex>
 
+#include "api_common.h"
 #include "rheo.h"
 #include "rheo_state.h"
 #include "team_words.h"
@@ -19,6 +20,10 @@ using namespace rheo;
 namespace {
 
 thread_local std::string g_err;
+
+}  // namespace
+
+namespace rheo {
 
 int fail(int code, const char* fmt, ...) {
     char buf[512];
@@ -33,6 +38,16 @@ int fail(int code, const char* fmt, ...) {
 int hip_fail(hipError_t e, const char* what) {
     return fail(RHEO_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+int check_ptr(const void* p, const char* name) {
+    if (!p) return fail(RHEO_EINVAL, "%s is NULL", name);
+    if ((uintptr_t)p % 16) return fail(RHEO_EINVAL, "%s is not 16-byte aligned", name);
+    return RHEO_OK;
+}
+
+}  // namespace rheo
+
+namespace {
 
 enum State { CREATED, EXPANDING, EXPANDED, PRUNED, VERIFIED };
 
@@ -91,12 +106,6 @@ int dalloc(rheo_tree* t, T** p, size_t count) {
 void free_all(rheo_tree* t) {
     for (int i = 0; i < t->nblocks; ++i) (void)hipFree(t->blocks[i]);
     t->nblocks = 0;
-}
-
-int check_ptr(const void* p, const char* name) {
-    if (!p) return fail(RHEO_EINVAL, "%s is NULL", name);
-    if ((uintptr_t)p % 16) return fail(RHEO_EINVAL, "%s is not 16-byte aligned", name);
-    return RHEO_OK;
 }
 
 int check_T(float T) {

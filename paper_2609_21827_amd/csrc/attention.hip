@@ -1,0 +1,693 @@
+// Attention of a drafted tree's rows over the paged cache (rheo_tree_attention).
+//
+// o_i = sum_j p_ij v_j with p = softmax_j(scale q_i.k_j), in one pass over the
+// entries with a running maximum and sum.  The g = heads / kv_heads query heads
+// of a key head read the same entries, so a sequence's rows and these heads
+// together are the M = n * g rows of one product, and every entry is read
+// once for up to 256 of them.
+//
+// Both products run on the matrix cores transposed, S^T = K Q^T and O^T = V^T
+// P^T, as 32x32x16 tiles: a lane's S^T values all belong to one row (column
+// lane % 32), so the softmax needs one exchange, between the two halves of the
+// wave, and its result is the second product's right operand as it stands:
+// lane h*32 + c holds S^T rows 8i + 4h + (0..3) of column c, and numbering the
+// second product's inner index 8h + j <-> entry (j < 4 ? 4h + j : 4 + 4h + j)
+// of each 16 makes those its values.  V^T comes from row-major V by LDS reads that
+// transpose 4x16 blocks (ds_read_b64_tr_b16) in the same numbering.
+//
+// Work is cut by tiles, not by sequences: the tiles of all (sequence, key
+// head, block of rows) items form one line, cut into equal stretches, one a
+// workgroup.  So lengths may differ at will.  An item that a cut goes through
+// leaves partial results (fp32, with maximum and sum), which k_attn_join
+// adds up.
+#include <type_traits>
+
+#include "cache_state.h"
+#include "half_types.h"
+
+namespace rheo {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// A launch's shape: DT head elements (head_dim padded), RT blocks of 32 rows
+// and NW waves to a workgroup; NW / RT waves share the entries of a tile, U
+// blocks of 32 of them each.
+template <int DT_, int RT_, int NW_, int U_>
+struct Shape {
+    static constexpr int DT = DT_, RT = RT_, NW = NW_, U = U_;
+    static constexpr int KW = NW / RT;               // waves to a row block
+    static constexpr int KT = 32 * KW * U;           // entries of a tile
+    static constexpr int ROWS = 32 * RT;
+    static constexpr int NT = 64 * NW;
+    static constexpr int KS = DT / 16, DB = DT / 32; // steps of QK, blocks of O's columns
+    // LDS rows: 16 bytes more than K's data spread a column's 16-byte reads over
+    // the banks, 64 more than V's the 4x16 blocks of the transposing reads
+    static constexpr int KROW = DT * 2 + 16, VROW = DT * 2 + 64;
+    static constexpr int CH = DT / 8;                // 16-byte vectors of a row
+    static constexpr int LOADS = KT * CH / NT;       // of K, and of V, a thread
+    static constexpr int LDS_KV = KT * (KROW + VROW);
+    static constexpr int LDS_OUT = KW > 1 ? (NW - RT) * 64 * DB * 16 * 4 : 0;
+    static constexpr int LDS = LDS_KV > LDS_OUT ? LDS_KV : LDS_OUT;
+    // a partial result: O^T as the lanes hold it, then maximum and sum of each row
+    static constexpr int PART = ROWS * DT + 2 * ROWS;
+    static_assert(KT * CH % NT == 0 && NW % RT == 0, "shape");
+};
+
+struct AttnArgs {
+    CacheDev c;
+    rheo_attention_args a;
+    int g;                         // query heads of a key head
+    int groups;                    // most stretches (workgroups)
+    int min_tiles;                 // fewest tiles of a stretch
+    int* desc;                     // [groups][8]: what k_attn_join adds up
+};
+
+// A sequence's part of the line.
+struct Seq {
+    int len, rows, tail, nrb;      // prefix, rows there, entries behind it, row blocks
+    int entries;                   // len + tail
+};
+
+template <typename S>
+__device__ __forceinline__ Seq seq_of(const AttnArgs& p, int b) {
+    Seq s;
+    const int64_t room = (int64_t)p.c.width << p.c.page_shift;
+    s.len = p.a.lens[b];
+    s.rows = p.a.count ? p.a.count[b] : p.a.n;
+    s.rows = min(max(s.rows, 0), p.a.n);
+    s.tail = max(p.a.tail - (p.a.n - s.rows), 0);
+    if (s.len < 0 || s.len + (int64_t)s.tail > room) {
+        if (s.rows) atomicOr(p.c.err, CE_TABLE);
+        s.len = (int)min((int64_t)max(s.len, 0), room);
+        s.tail = (int)min((int64_t)s.tail, room - s.len);
+    }
+    s.entries = s.len + s.tail;
+    s.nrb = (s.rows * p.g + S::ROWS - 1) / S::ROWS;
+    return s;
+}
+
+// Tiles of row block rb, at least one: without a mask no row attends past what
+// its last row does.
+template <typename S>
+__device__ __forceinline__ int tiles_of(const AttnArgs& p, const Seq& s, int rb) {
+    int end = s.entries;
+    if (!p.a.mask) {
+        const int last = min(((rb + 1) * S::ROWS - 1) / p.g, s.rows - 1);
+        end = min(end, s.len + last + p.a.tail - p.a.n + 1);
+    }
+    return max((end + S::KT - 1) / S::KT, 1);
+}
+
+// ... of all row blocks, for one key head
+template <typename S>
+__device__ __forceinline__ int64_t tiles_of_head(const AttnArgs& p, const Seq& s) {
+    if (p.a.mask) return (int64_t)s.nrb * tiles_of<S>(p, s, 0);
+    int64_t t = 0;
+    for (int rb = 0; rb < s.nrb; ++rb) t += tiles_of<S>(p, s, rb);
+    return t;
+}
+
+// Stretch w of the line: tiles [t0, t1) of it, the sequence that t0 is in and
+// the tiles before that sequence.  All threads of the block call it.
+struct Stretch {
+    int64_t total, t0, t1, before;
+    int groups, seq;
+};
+
+__device__ __forceinline__ int64_t stretch_start(int64_t total, int groups, int w) {
+    return total * w / groups;
+}
+
+template <typename S>
+__device__ Stretch find_stretch(const AttnArgs& p, int w) {
+    __shared__ int64_t s_wave[S::NW], s_before;
+    __shared__ int s_seq;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, B = p.c.B;
+    const int per = (B + S::NT - 1) / S::NT, b0 = min(tid * per, B), b1 = min(b0 + per, B);
+    int64_t mine = 0;
+    for (int b = b0; b < b1; ++b) mine += p.c.K * tiles_of_head<S>(p, seq_of<S>(p, b));
+    int64_t incl = mine;
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t u = __shfl_up(incl, o);
+        if (lane >= o) incl += u;
+    }
+    if (lane == 63) s_wave[wave] = incl;
+    __syncthreads();
+    int64_t excl = incl - mine, total = 0;
+    for (int v = 0; v < S::NW; ++v) {
+        if (v < wave) excl += s_wave[v];
+        total += s_wave[v];
+    }
+    Stretch r;
+    r.total = total;
+    const int64_t most = (total + p.min_tiles - 1) / p.min_tiles;
+    r.groups = (int)(most < p.groups ? most : p.groups);
+    if (w >= r.groups) {
+        r.t0 = r.t1 = 0;
+        return r;
+    }
+    r.t0 = stretch_start(total, r.groups, w);
+    r.t1 = stretch_start(total, r.groups, w + 1);
+    if (r.t0 >= excl && r.t0 < excl + mine) {
+        int64_t t = excl;
+        for (int b = b0; b < b1; ++b) {
+            const int64_t k = p.c.K * tiles_of_head<S>(p, seq_of<S>(p, b));
+            if (r.t0 < t + k) {
+                s_seq = b;
+                s_before = t;
+                break;
+            }
+            t += k;
+        }
+    }
+    __syncthreads();
+    r.seq = __builtin_amdgcn_readfirstlane(s_seq);
+    r.before = s_before;
+    return r;
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) s16x4* lds_s4;
+
+template <typename T>
+__device__ __forceinline__ f32x16 mfma(const u32x4& a, const u32x4& b, const f32x16& c) {
+    typedef typename Pack<T>::v8 v8;
+    if constexpr (std::is_same<T, __bf16>::value)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8, a),
+                                                       __builtin_bit_cast(v8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8, a),
+                                                      __builtin_bit_cast(v8, b), c, 0, 0, 0);
+}
+
+// A value of the lane's own and of the other half's lane of the same column.
+__device__ __forceinline__ f32x2 both_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                    false);
+    return f32x2{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+
+template <typename T>
+__device__ __forceinline__ bool any_unfinite(const uint4& v) {
+    constexpr uint32_t E = Pack<T>::kExp, E2 = E | E << 16;
+    bool bad = false;
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t e = w[i] & E2;
+        bad |= (e & 0xFFFFu) == E || (e >> 16) == E;
+    }
+    return bad;
+}
+
+// What a row block's waves hold while they go through an item's tiles.
+template <typename S>
+struct Rows {
+    u32x4 q[S::KS];                // Q^T: the lane's row, elements 16s + 8h + (0..7)
+    f32x16 o[S::DB];               // O^T: row, elements 32db + 8(r/4) + 4h + r%4
+    float m, l;                    // its maximum score so far; its half's sum
+};
+
+}  // namespace
+
+template <typename T, typename S>
+__global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention(AttnArgs p) {
+    extern __shared__ __align__(16) char s_lds[];
+    __shared__ float s_ml[S::KW > 1 ? S::NW * 64 : 2];
+    __shared__ uint32_t s_bad[2][S::KT / 32];
+    char* const s_k = s_lds;
+    char* const s_v = s_lds + S::KT * S::KROW;
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rt = wave % S::RT, kw = wave / S::RT;
+    const CacheDev& c = p.c;
+    const rheo_attention_args& a = p.a;
+    const int w = blockIdx.x, D = c.D;
+    const float to2 = a.scale * kLog2e;              // scores to exponents of 2
+    if (tid < 2 * (S::KT / 32)) (&s_bad[0][0])[tid] = 0;
+
+    const Stretch st = find_stretch<S>(p, w);
+    if (st.t0 >= st.t1) {
+        if (tid == 0) p.desc[8 * w] = 0;
+        return;
+    }
+    // the first item
+    int b = st.seq;
+    Seq sq = seq_of<S>(p, b);
+    int64_t rel = st.t0 - st.before;
+    const int64_t per_head = tiles_of_head<S>(p, sq);
+    int hk = (int)(rel / per_head), rb = 0;
+    rel -= hk * per_head;
+    while (rel >= tiles_of<S>(p, sq, rb)) rel -= tiles_of<S>(p, sq, rb++);
+    int tile = (int)rel;                                 // the item's tile to begin with
+    int64_t left = st.t1 - st.t0;
+    {
+        // the join of the first item, by the first cut inside it
+        const int64_t begins = st.t0 - tile, ends = begins + tiles_of<S>(p, sq, rb);
+        if (tid == 0) {
+            int* d = p.desc + 8 * w;
+            const bool mine = tile > 0 && stretch_start(st.total, st.groups, w - 1) <= begins;
+            d[0] = 0;
+            if (mine) {
+                int n = 2;
+                while (stretch_start(st.total, st.groups, w + n - 1) < ends) ++n;
+                d[0] = n;                            // partial results
+                d[1] = 2 * (w - 1) + (stretch_start(st.total, st.groups, w - 1) < begins ? 1 : 0);
+                d[2] = b;
+                d[3] = hk;
+                d[4] = rb;
+            }
+        }
+    }
+
+    uint4 kr[S::LOADS], vr[S::LOADS];
+    int pid[S::LOADS];
+    int turn = 0;                                    // which of s_bad the tile at hand has
+    for (bool first = true; left > 0; first = false) {
+        const int tiles = tiles_of<S>(p, sq, rb);
+        const int end_tile = (int)min((int64_t)tiles, tile + left);
+        const int32_t* row_table = a.table + (int64_t)b * c.width;
+        const int64_t head = (int64_t)hk * D;
+        const int entries = sq.entries, len = sq.len;
+
+        // the pages of a tile's entries, and the entries
+        auto fetch_pages = [&](int t) {
+#pragma unroll
+            for (int v = 0; v < S::LOADS; ++v) {
+                const int row = (tid + v * S::NT) / S::CH;
+                const int e = min(t * S::KT + row, entries - 1);
+                int page = entries > 0 ? row_table[e >> c.page_shift] : 0;
+                if ((unsigned)page >= (unsigned)c.pages) {
+                    atomicOr(c.err, CE_PAGE);
+                    page = 0;
+                }
+                pid[v] = page;
+            }
+        };
+        auto fetch = [&](int t) {
+            const bool part = (t + 1) * S::KT > entries || D < S::DT;
+#pragma unroll
+            for (int v = 0; v < S::LOADS; ++v) {
+                const int idx = tid + v * S::NT, row = idx / S::CH, ch = idx % S::CH;
+                int e = t * S::KT + row;
+                const bool in = e < entries && ch * 8 < D;
+                e = max(min(e, entries - 1), 0);
+                const int64_t at = pid[v] * c.page_stride +
+                                   (int64_t)(e & ((1 << c.page_shift) - 1)) * (c.K * D) + head +
+                                   min(ch * 8, D - 8);
+                kr[v] = *(const uint4*)((const T*)a.k_cache + at);
+                vr[v] = *(const uint4*)((const T*)a.v_cache + at);
+                if (part && !in) kr[v] = vr[v] = make_uint4(0, 0, 0, 0);
+            }
+        };
+
+        Rows<S> x;
+        const int r = rb * S::ROWS + rt * 32 + col;  // the lane's row of the item
+        const bool live = r < sq.rows * p.g;
+        const int qi = live ? r / p.g : 0, qh = hk * p.g + (live ? r - qi * p.g : 0);
+        const int64_t qrow = (int64_t)b * a.n + qi;
+        {
+            const T* q = (const T*)a.q + qrow * a.q_stride + (int64_t)qh * D;
+#pragma unroll
+            for (int s = 0; s < S::KS; ++s) {
+                const int d = 16 * s + 8 * half;
+                x.q[s] = u32x4{0, 0, 0, 0};
+                if (live && d < D) x.q[s] = *(const u32x4*)(q + d);
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < S::DB; ++d) x.o[d] = 0.0f;
+        x.m = -INFINITY;
+        x.l = 0.0f;
+        const uint8_t* mrow = a.mask ? a.mask + qrow * a.tail : nullptr;
+        const int reach = qi + a.tail - a.n;         // without a mask: tail entries seen, less 1
+
+        fetch_pages(tile);
+        fetch(tile);
+        if (tile + 1 < end_tile) fetch_pages(tile + 1);
+        for (int t = tile; t < end_tile; ++t) {
+            __syncthreads();                         // the tile before has been read
+            const bool tail_tile = (t + 1) * S::KT > len;
+#pragma unroll
+            for (int v = 0; v < S::LOADS; ++v) {
+                const int idx = tid + v * S::NT, row = idx / S::CH, ch = idx % S::CH;
+                *(uint4*)(s_k + row * S::KROW + ch * 16) = kr[v];
+                // An entry that some row does not attend must not reach it: 0 * inf
+                // is not 0.  Such vectors go in as zeros and are added by hand.
+                if (tail_tile && any_unfinite<T>(vr[v])) {
+                    vr[v] = make_uint4(0, 0, 0, 0);
+                    atomicOr(&s_bad[turn][row / 32], 1u << (row % 32));
+                }
+                *(uint4*)(s_v + row * S::VROW + ch * 16) = vr[v];
+            }
+            __syncthreads();
+            if (tid < S::KT / 32) s_bad[turn ^ 1][tid] = 0;
+            if (t + 1 < end_tile) fetch(t + 1);
+            if (t + 2 < end_tile) fetch_pages(t + 2);
+
+            // S^T of the wave's U blocks of 32 entries
+            const int e0 = kw * S::U * 32;           // (of the tile)
+            f32x16 sc[S::U];
+#pragma unroll
+            for (int u = 0; u < S::U; ++u) {
+                sc[u] = 0.0f;
+                const char* kp = s_k + (e0 + u * 32 + col) * S::KROW + half * 16;
+#pragma unroll
+                for (int s = 0; s < S::KS; ++s)
+                    sc[u] = mfma<T>(*(const u32x4*)(kp + s * 32), x.q[s], sc[u]);
+            }
+            if (tail_tile) {
+                const int eh = t * S::KT + e0 + 4 * half;
+                if (mrow && sq.tail > 0) {
+#pragma unroll
+                    for (int u = 0; u < S::U; ++u) {
+                        uint8_t named[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            named[i] = mrow[min(max(eh + u * 32 + 8 * (i / 4) + i % 4 - len, 0),
+                                                sq.tail - 1)];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int e = eh + u * 32 + 8 * (i / 4) + i % 4;
+                            const bool seen = (e < len) | ((e < entries) & (named[i] != 0));
+                            sc[u][i] = seen ? sc[u][i] : -INFINITY;
+                        }
+                    }
+                } else {
+                    const int end = mrow ? entries : min(len + reach + 1, entries);
+#pragma unroll
+                    for (int u = 0; u < S::U; ++u)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            sc[u][i] = eh + u * 32 + 8 * (i / 4) + i % 4 < end ? sc[u][i] : -INFINITY;
+                }
+            }
+            // running maximum and sum
+            float mx = sc[0][0];
+#pragma unroll
+            for (int u = 0; u < S::U; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[u][i]);
+            const f32x2 mb = both_halves(mx);
+            const float m = fmaxf(x.m, fmaxf(mb[0], mb[1]));
+            const float ref = m == -INFINITY ? 0.0f : m * to2;
+            if (__any(m > x.m)) {
+                const float f = __builtin_amdgcn_exp2f(__fmaf_rn(x.m, to2, -ref));
+                x.l *= f;
+#pragma unroll
+                for (int d = 0; d < S::DB; ++d) x.o[d] *= f;
+            }
+            x.m = m;
+            float sum = 0.0f;
+#pragma unroll
+            for (int u = 0; u < S::U; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    sc[u][i] = __builtin_amdgcn_exp2f(__fmaf_rn(sc[u][i], to2, -ref));
+                    sum += sc[u][i];
+                }
+            x.l += sum;
+            // O^T += V^T P^T
+#pragma unroll
+            for (int u = 0; u < S::U; ++u)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    u32x4 pt;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        pt[i] = pack2<T>(sc[u][8 * k + 2 * i], sc[u][8 * k + 2 * i + 1]);
+                    const char* vp = s_v + (e0 + u * 32 + 16 * k + 4 * half + (lane & 15) / 4) * S::VROW +
+                                     (16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
+#pragma unroll
+                    for (int d = 0; d < S::DB; ++d) {
+                        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(vp + d * 64));
+                        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                            (lds_s4)(vp + d * 64 + 8 * S::VROW));
+                        const s16x8 va = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                        x.o[d] = mfma<T>(__builtin_bit_cast(u32x4, va), pt, x.o[d]);
+                    }
+                }
+            // the entries left out above, added where they are attended
+            if (tail_tile) {
+#pragma unroll
+                for (int u = 0; u < S::U; ++u) {
+                    uint32_t bad = __builtin_amdgcn_readfirstlane(s_bad[turn][e0 / 32 + u]);
+                    while (bad) {
+                        const int k = __builtin_ctz(bad);
+                        bad &= bad - 1;
+                        float pk = 0.0f;             // in half (k / 4) % 2, register 4(k/8) + k%4
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (i == 4 * (k / 8) + k % 4) pk = sc[u][i];
+                        const f32x2 pb = both_halves(pk);
+                        pk = (k / 4) % 2 ? pb[1] : pb[0];
+                        const int e = t * S::KT + e0 + u * 32 + k;
+                        const int page = min(max(row_table[e >> c.page_shift], 0), c.pages - 1);
+                        const T* v = (const T*)a.v_cache + page * c.page_stride +
+                                     (int64_t)(e & ((1 << c.page_shift) - 1)) * (c.K * D) + head;
+#pragma unroll
+                        for (int d = 0; d < S::DB; ++d)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                // (selects, not branches, around an accumulator's elements)
+                                const int at = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
+                                const int in = min(at, D - 1);
+                                const bool add = (at < D) & (pk != 0.0f) &
+                                                 any_unfinite<T>(*(const uint4*)(v + (in & ~7)));
+                                const float sum = __fmaf_rn(pk, (float)v[in], x.o[d][i]);
+                                x.o[d][i] = add ? sum : x.o[d][i];
+                            }
+                    }
+                }
+            }
+            turn ^= 1;
+        }
+
+        // the waves of a row block put together
+        const f32x2 lb = both_halves(x.l);
+        x.l = lb[0] + lb[1];
+        if constexpr (S::KW > 1) {
+            if (!half) {
+                s_ml[(wave * 32 + col) * 2] = x.m;
+                s_ml[(wave * 32 + col) * 2 + 1] = x.l;
+            }
+            __syncthreads();
+            float m = -INFINITY, l = 0.0f;
+#pragma unroll
+            for (int k = 0; k < S::KW; ++k) m = fmaxf(m, s_ml[((k * S::RT + rt) * 32 + col) * 2]);
+            const float ref = m == -INFINITY ? 0.0f : m * to2;
+#pragma unroll
+            for (int k = 0; k < S::KW; ++k) {
+                const float* ml = s_ml + ((k * S::RT + rt) * 32 + col) * 2;
+                l += ml[1] * __builtin_amdgcn_exp2f(__fmaf_rn(ml[0], to2, -ref));
+            }
+            const float f = __builtin_amdgcn_exp2f(__fmaf_rn(x.m, to2, -ref));
+            float* out = (float*)s_lds;
+#pragma unroll
+            for (int d = 0; d < S::DB; ++d) {
+                x.o[d] *= f;
+                if (kw > 0)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        out[(((wave - S::RT) * S::DB + d) * 16 + i) * 64 + lane] = x.o[d][i];
+            }
+            __syncthreads();
+            if (kw == 0)
+#pragma unroll 1
+                for (int k = 1; k < S::KW; ++k)
+#pragma unroll
+                    for (int d = 0; d < S::DB; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            x.o[d][i] += out[((((k - 1) * S::RT + rt) * S::DB + d) * 16 + i) * 64 + lane];
+            x.m = m;
+            x.l = l;
+        }
+        if (kw == 0) {
+            if (tile == 0 && end_tile == tiles) {
+                const float inv = x.l == 0.0f ? 0.0f : 1.0f / x.l;
+                T* o = (T*)a.out + qrow * a.out_stride + (int64_t)qh * D;
+                if (live) {
+#pragma unroll
+                    for (int d = 0; d < S::DB; ++d)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int at = 32 * d + 8 * i + 4 * half;
+                            if (at < D)
+                                *(uint2*)(o + at) = make_uint2(
+                                    pack2<T>(x.o[d][4 * i] * inv, x.o[d][4 * i + 1] * inv),
+                                    pack2<T>(x.o[d][4 * i + 2] * inv, x.o[d][4 * i + 3] * inv));
+                        }
+                    if (a.lse && !half) a.lse[qrow * c.H + qh] = x.m * a.scale + logf(x.l);
+                }
+            } else {
+                float* part = c.part + (int64_t)(2 * w + (first ? 0 : 1)) * S::PART;
+#pragma unroll
+                for (int d = 0; d < S::DB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        part[((rt * S::DB + d) * 16 + i) * 64 + lane] = x.o[d][i];
+                if (!half) {
+                    float* ml = part + S::ROWS * S::DT + (rt * 32 + col) * 2;
+                    ml[0] = x.m;
+                    ml[1] = x.l;
+                }
+            }
+        }
+        // the next item
+        left -= end_tile - tile;
+        tile = 0;
+        if (++rb == sq.nrb) {
+            rb = 0;
+            if (++hk == c.K) {
+                hk = 0;
+                if (left > 0) {
+                    do { sq = seq_of<S>(p, ++b); } while (sq.nrb == 0);
+                }
+            }
+        }
+    }
+}
+
+// The partial results of one cut item added up: block x of a launch has the item
+// that begins at cut x's left (see k_tree_attention), block y its 32 rows and
+// 32 elements; a wave takes eight of these, in pairs of the lanes' halves.
+template <typename T, typename S>
+__global__ __launch_bounds__(256) void k_attn_join(AttnArgs p) {
+    const int* desc = p.desc + 8 * blockIdx.x;
+    const int n = desc[0];
+    if (n == 0) return;
+    const int slot0 = desc[1], b = desc[2], hk = desc[3], rb = desc[4];
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5, i = threadIdx.x >> 6;
+    const int rt = blockIdx.y / S::DB, d = blockIdx.y % S::DB;
+    const rheo_attention_args& a = p.a;
+    const CacheDev& c = p.c;
+    const Seq sq = seq_of<S>(p, b);
+    const int r = rb * S::ROWS + rt * 32 + col;
+    const int at = 32 * d + 8 * i + 4 * half;
+    if (r >= sq.rows * p.g || at >= c.D) return;
+    // (slot0 is the first stretch's, maybe its second; the others' first)
+    const int w0 = slot0 >> 1;
+    auto part = [&](int k) { return c.part + (int64_t)(k ? 2 * (w0 + k) : slot0) * S::PART; };
+    const int ml = S::ROWS * S::DT + (rt * 32 + col) * 2;
+    const int oi = ((rt * S::DB + d) * 16 + 4 * i) * 64 + lane;
+    const float to2 = a.scale * kLog2e;
+    float m = -INFINITY;
+    for (int k = 0; k < n; ++k) m = fmaxf(m, part(k)[ml]);
+    const float ref = m == -INFINITY ? 0.0f : m * to2;
+    float l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k = 0; k < n; ++k) {
+        const float* q = part(k);
+        const float f = __builtin_amdgcn_exp2f(__fmaf_rn(q[ml], to2, -ref));
+        l = __fmaf_rn(q[ml + 1], f, l);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = __fmaf_rn(q[oi + 64 * e], f, o[e]);
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int qi = r / p.g, qh = hk * p.g + r - qi * p.g;
+    const int64_t qrow = (int64_t)b * a.n + qi;
+    T* out = (T*)a.out + qrow * a.out_stride + (int64_t)qh * c.D + at;
+    *(uint2*)out = make_uint2(pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv));
+    if (a.lse && at == 0) a.lse[qrow * c.H + qh] = m * a.scale + logf(l);
+}
+
+namespace {
+
+// Shapes for up to 32, 64, 128 and more rows of an item.
+template <int DT>
+struct Shapes;
+template <>
+struct Shapes<64> {
+    typedef Shape<64, 1, 4, 1> R1;
+    typedef Shape<64, 2, 4, 1> R2;
+    typedef Shape<64, 4, 4, 2> R4;
+    typedef Shape<64, 8, 8, 2> R8;
+};
+template <>
+struct Shapes<128> {
+    typedef Shape<128, 1, 4, 1> R1;
+    typedef Shape<128, 2, 4, 1> R2;
+    typedef Shape<128, 4, 4, 2> R4;
+    typedef Shape<128, 8, 8, 2> R8;
+};
+template <>
+struct Shapes<256> {
+    typedef Shape<256, 1, 4, 1> R1;
+    typedef Shape<256, 2, 4, 1> R2;
+    typedef Shape<256, 4, 4, 1> R4;
+    typedef R4 R8;
+};
+
+// Workgroups a compute unit holds at once.
+template <typename S>
+constexpr int resident() {
+    return S::DT > 128 || S::NW > 4 ? 1 : 2;
+}
+
+template <typename S>
+size_t part_floats(int units) {
+    return (size_t)units * resident<S>() * 2 * S::PART;
+}
+
+template <int DT>
+size_t workspace(int units) {
+    typedef Shapes<DT> H;
+    size_t n = part_floats<typename H::R1>(units);
+    const size_t r2 = part_floats<typename H::R2>(units), r4 = part_floats<typename H::R4>(units),
+                 r8 = part_floats<typename H::R8>(units);
+    n = n > r2 ? n : r2;
+    n = n > r4 ? n : r4;
+    return n > r8 ? n : r8;
+}
+
+template <typename T, typename S>
+hipError_t start(AttnArgs p, hipStream_t s) {
+    static_assert(S::LDS <= 160 * 1024 - 4096, "LDS");
+    p.groups = p.c.slots * resident<S>();
+    p.min_tiles = 1;
+    const void* fn = (const void*)k_tree_attention<T, S>;
+    hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+    if (e != hipSuccess) return e;
+    k_tree_attention<T, S><<<p.groups, S::NT, S::LDS, s>>>(p);
+    k_attn_join<T, S><<<dim3(p.groups, S::RT * S::DB), 256, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+template <typename T, int DT>
+hipError_t start_rows(const AttnArgs& p, hipStream_t s) {
+    typedef Shapes<DT> H;
+    const int64_t rows = (int64_t)p.a.n * p.g;
+    if (rows <= 32) return start<T, typename H::R1>(p, s);
+    if (rows <= 64) return start<T, typename H::R2>(p, s);
+    if (rows <= 128 || DT > 128) return start<T, typename H::R4>(p, s);
+    return start<T, typename H::R8>(p, s);
+}
+
+template <typename T>
+hipError_t start_dim(const AttnArgs& p, hipStream_t s) {
+    if (p.c.D <= 64) return start_rows<T, 64>(p, s);
+    if (p.c.D <= 128) return start_rows<T, 128>(p, s);
+    return start_rows<T, 256>(p, s);
+}
+
+}  // namespace
+
+size_t attention_workspace(const CacheDev& c) {
+    const size_t n = c.D <= 64 ? workspace<64>(c.slots) : c.D <= 128 ? workspace<128>(c.slots)
+                                                                     : workspace<256>(c.slots);
+    return n + (size_t)c.slots * 2 * 8;      // and the descriptions of the joins
+}
+
+hipError_t launch_tree_attention(const CacheDev& c, const rheo_attention_args& a, hipStream_t s) {
+    AttnArgs p{};
+    p.c = c;
+    p.a = a;
+    p.g = c.H / c.K;
+    p.desc = (int*)(c.part + attention_workspace(c) - (size_t)c.slots * 2 * 8);
+    return c.dtype == RHEO_BF16 ? start_dim<__bf16>(p, s) : start_dim<_Float16>(p, s);
+}
+
+}  // namespace rheo
