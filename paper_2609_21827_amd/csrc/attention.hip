@@ -51,7 +51,7 @@ struct Shape {
     static constexpr int LDS_OUT = KW > 1 ? (NW - RT) * 64 * DB * 16 * 4 : 0;
     static constexpr int LDS = LDS_KV > LDS_OUT ? LDS_KV : LDS_OUT;
     // a partial result: O^T as the lanes hold it, then maximum and sum of each row
-    static constexpr int PART = ROWS * DT + 2 * ROWS;
+    static constexpr int PART = ROWS * DT + 2 * ROWS + 64;    // (and a flag)
     static_assert(KT * CH % NT == 0 && NW % RT == 0, "shape");
 };
 
@@ -190,17 +190,48 @@ __device__ __forceinline__ f32x2 both_halves(float x) {
     return f32x2{__uint_as_float(r[0]), __uint_as_float(r[1])};
 }
 
+// Elements that are infinite or NaN made 0; whether there was one.
 template <typename T>
-__device__ __forceinline__ bool any_unfinite(const uint4& v) {
-    constexpr uint32_t E = Pack<T>::kExp, E2 = E | E << 16;
+__device__ __forceinline__ bool drop_unfinite(uint4& v) {
+    constexpr uint32_t E = Pack<T>::kExp;
     bool bad = false;
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t* w = &v.x;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t e = w[i] & E2;
-        bad |= (e & 0xFFFFu) == E || (e >> 16) == E;
+        const bool lo = (w[i] & E) == E, hi = (w[i] & E << 16) == E << 16;
+        w[i] = (lo ? 0 : w[i] & 0xFFFFu) | (hi ? 0 : w[i] & 0xFFFF0000u);
+        bad |= lo | hi;
     }
     return bad;
+}
+
+// The infinite and NaN values of entries behind the prefix, which the products
+// left out, added to an output row that attends them: `at` and the three
+// elements behind it of each of the lane's fours, 8 apart.  Their
+// probabilities are not 0, so the values themselves decide.  Rare and slow; by the
+// lanes that wrote the row.
+template <typename T>
+__device__ __forceinline__ void add_unfinite(const AttnArgs& p, int b, int hk, const Seq& sq, int qi,
+                                             T* out, int at, int step) {
+    const CacheDev& c = p.c;
+    const int64_t qrow = (int64_t)b * p.a.n + qi;
+#pragma unroll 1
+    for (int j = 0; j < sq.tail; ++j) {
+        const bool seen = p.a.mask ? p.a.mask[qrow * p.a.tail + j] != 0 : j <= qi + p.a.tail - p.a.n;
+        if (!seen) continue;
+        const int e = sq.len + j;
+        int page = p.a.table[(int64_t)b * c.width + (e >> c.page_shift)];
+        page = min(max(page, 0), c.pages - 1);
+        const T* v = (const T*)p.a.v_cache + page * c.page_stride +
+                     ((int64_t)(e & ((1 << c.page_shift) - 1)) * c.K + hk) * c.D;
+#pragma unroll 1
+        for (int d = at; d < c.D; d += step)
+#pragma unroll 1
+            for (int i = d; i < d + 4; ++i) {
+                const float x = (float)v[i];
+                if (!(fabsf(x) < INFINITY)) out[i] = (T)((float)out[i] + x);
+            }
+    }
 }
 
 // What a row block's waves hold while they go through an item's tiles.
@@ -217,7 +248,7 @@ template <typename T, typename S>
 __global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention(AttnArgs p) {
     extern __shared__ __align__(16) char s_lds[];
     __shared__ float s_ml[S::KW > 1 ? S::NW * 64 : 2];
-    __shared__ uint32_t s_bad[2][S::KT / 32];
+    __shared__ int s_bad;                            // values left out of the item's products
     char* const s_k = s_lds;
     char* const s_v = s_lds + S::KT * S::KROW;
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
@@ -227,7 +258,7 @@ __global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention
     const rheo_attention_args& a = p.a;
     const int w = blockIdx.x, D = c.D;
     const float to2 = a.scale * kLog2e;              // scores to exponents of 2
-    if (tid < 2 * (S::KT / 32)) (&s_bad[0][0])[tid] = 0;
+    if (tid == 0) s_bad = 0;
 
     const Stretch st = find_stretch<S>(p, w);
     if (st.t0 >= st.t1) {
@@ -265,7 +296,6 @@ __global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention
 
     uint4 kr[S::LOADS], vr[S::LOADS];
     int pid[S::LOADS];
-    int turn = 0;                                    // which of s_bad the tile at hand has
     for (bool first = true; left > 0; first = false) {
         const int tiles = tiles_of<S>(p, sq, rb);
         const int end_tile = (int)min((int64_t)tiles, tile + left);
@@ -336,15 +366,11 @@ __global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention
                 const int idx = tid + v * S::NT, row = idx / S::CH, ch = idx % S::CH;
                 *(uint4*)(s_k + row * S::KROW + ch * 16) = kr[v];
                 // An entry that some row does not attend must not reach it: 0 * inf
-                // is not 0.  Such vectors go in as zeros and are added by hand.
-                if (tail_tile && any_unfinite<T>(vr[v])) {
-                    vr[v] = make_uint4(0, 0, 0, 0);
-                    atomicOr(&s_bad[turn][row / 32], 1u << (row % 32));
-                }
+                // is not 0.  Such values go in as zeros and are added at the end.
+                if (tail_tile && t * S::KT + row >= len && drop_unfinite<T>(vr[v])) s_bad = 1;
                 *(uint4*)(s_v + row * S::VROW + ch * 16) = vr[v];
             }
             __syncthreads();
-            if (tid < S::KT / 32) s_bad[turn ^ 1][tid] = 0;
             if (t + 1 < end_tile) fetch(t + 1);
             if (t + 2 < end_tile) fetch_pages(t + 2);
 
@@ -430,40 +456,6 @@ __global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention
                         x.o[d] = mfma<T>(__builtin_bit_cast(u32x4, va), pt, x.o[d]);
                     }
                 }
-            // the entries left out above, added where they are attended
-            if (tail_tile) {
-#pragma unroll
-                for (int u = 0; u < S::U; ++u) {
-                    uint32_t bad = __builtin_amdgcn_readfirstlane(s_bad[turn][e0 / 32 + u]);
-                    while (bad) {
-                        const int k = __builtin_ctz(bad);
-                        bad &= bad - 1;
-                        float pk = 0.0f;             // in half (k / 4) % 2, register 4(k/8) + k%4
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (i == 4 * (k / 8) + k % 4) pk = sc[u][i];
-                        const f32x2 pb = both_halves(pk);
-                        pk = (k / 4) % 2 ? pb[1] : pb[0];
-                        const int e = t * S::KT + e0 + u * 32 + k;
-                        const int page = min(max(row_table[e >> c.page_shift], 0), c.pages - 1);
-                        const T* v = (const T*)a.v_cache + page * c.page_stride +
-                                     (int64_t)(e & ((1 << c.page_shift) - 1)) * (c.K * D) + head;
-#pragma unroll
-                        for (int d = 0; d < S::DB; ++d)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                // (selects, not branches, around an accumulator's elements)
-                                const int at = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
-                                const int in = min(at, D - 1);
-                                const bool add = (at < D) & (pk != 0.0f) &
-                                                 any_unfinite<T>(*(const uint4*)(v + (in & ~7)));
-                                const float sum = __fmaf_rn(pk, (float)v[in], x.o[d][i]);
-                                x.o[d][i] = add ? sum : x.o[d][i];
-                            }
-                    }
-                }
-            }
-            turn ^= 1;
         }
 
         // the waves of a row block put together
@@ -506,6 +498,9 @@ __global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention
             x.m = m;
             x.l = l;
         }
+        const int bad = s_bad;
+        __syncthreads();
+        if (tid == 0) s_bad = 0;
         if (kw == 0) {
             if (tile == 0 && end_tile == tiles) {
                 const float inv = x.l == 0.0f ? 0.0f : 1.0f / x.l;
@@ -522,6 +517,7 @@ __global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention
                                     pack2<T>(x.o[d][4 * i + 2] * inv, x.o[d][4 * i + 3] * inv));
                         }
                     if (a.lse && !half) a.lse[qrow * c.H + qh] = x.m * a.scale + logf(x.l);
+                    if (bad) add_unfinite<T>(p, b, hk, sq, qi, o, 4 * half, 8);
                 }
             } else {
                 float* part = c.part + (int64_t)(2 * w + (first ? 0 : 1)) * S::PART;
@@ -535,6 +531,7 @@ __global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention
                     ml[0] = x.m;
                     ml[1] = x.l;
                 }
+                if (tid == 0) ((int*)part)[S::PART - 1] = bad;
             }
         }
         // the next item
@@ -579,8 +576,10 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs p) {
     for (int k = 0; k < n; ++k) m = fmaxf(m, part(k)[ml]);
     const float ref = m == -INFINITY ? 0.0f : m * to2;
     float l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    int bad = 0;
     for (int k = 0; k < n; ++k) {
         const float* q = part(k);
+        bad |= ((const int*)q)[S::PART - 1];
         const float f = __builtin_amdgcn_exp2f(__fmaf_rn(q[ml], to2, -ref));
         l = __fmaf_rn(q[ml + 1], f, l);
 #pragma unroll
@@ -589,9 +588,10 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs p) {
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     const int qi = r / p.g, qh = hk * p.g + r - qi * p.g;
     const int64_t qrow = (int64_t)b * a.n + qi;
-    T* out = (T*)a.out + qrow * a.out_stride + (int64_t)qh * c.D + at;
-    *(uint2*)out = make_uint2(pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv));
+    T* out = (T*)a.out + qrow * a.out_stride + (int64_t)qh * c.D;
+    *(uint2*)(out + at) = make_uint2(pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv));
     if (a.lse && at == 0) a.lse[qrow * c.H + qh] = m * a.scale + logf(l);
+    if (bad) add_unfinite<T>(p, b, hk, sq, qi, out, at, c.D);
 }
 
 namespace {

@@ -484,6 +484,24 @@ def test_infinite_values_reach_the_rows_that_attend_them(binding):
     s.cache.close()
 
 
+@pytest.mark.parametrize("n,H,K", [(20, 4, 2), (1, 4, 1), (61, 4, 1)])
+def test_infinite_values_of_the_prefix_reach_all_rows(binding, n, H, K):
+    """In the tile that the drafted entries begin in, in one before it, next to the last."""
+    s = Setup(binding, F16, [337], n, n, H, K, 64, 16, seed=4)
+    mask = _tree_mask(s.g, 1, n)
+    clean = s.run(mask)
+    for e, d in ((3, 5), (336, 17), (330, 40)):
+        s.vc.flatten(0, 1)[int(s.table[0, e // 16]) * 16 + e % 16, :, d] = math.inf
+    out, lse = s.run(mask)
+    assert torch.equal(lse, clean[1])
+    for d in range(64):
+        if d in (5, 17, 40):
+            assert (out[..., d] == math.inf).all()
+        else:
+            assert torch.equal(out[..., d], clean[0][..., d])
+    s.cache.close()
+
+
 def test_attention_flags_pages_outside_the_pool(binding):
     s = Setup(binding, BF16, [70], 3, 3, 4, 2, 64, 16)
     for bad in (-1, s.pages, 1 << 30):
