@@ -25,6 +25,10 @@ FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC",
          "-ffp-contract=off", "-fno-fast-math",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+# The default scheduler leaves every LDS read of the attention loop next to the
+# product that takes it; this one keeps the order that the loop asks for
+# (64 trees over 4096 tokens: 256 us against 287).
+SOURCE_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"]}
 
 
 def _run(cmd, verbose):
@@ -44,7 +48,7 @@ def _compile(out, sources, verbose, jobs=None):
     objs = [os.path.join(HERE, "build", os.path.basename(out) + "." + s + ".o") for s in sources]
     os.makedirs(os.path.join(HERE, "build"), exist_ok=True)
     with ThreadPoolExecutor(jobs or min(4, os.cpu_count() or 1)) as pool:
-        list(pool.map(lambda so: _run([HIPCC] + FLAGS + ["-c", os.path.join(CSRC, so[0]),
+        list(pool.map(lambda so: _run([HIPCC] + FLAGS + SOURCE_FLAGS.get(so[0], []) + ["-c", os.path.join(CSRC, so[0]),
                                                          "-o", so[1]], verbose),
                       zip(sources, objs)))
     _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", out + ".tmp"] + objs, verbose)

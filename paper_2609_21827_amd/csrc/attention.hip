@@ -33,26 +33,30 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 // A launch's shape: DT head elements (head_dim padded), RT blocks of 32 rows
 // and NW waves to a workgroup; NW / RT waves share the entries of a tile, U
-// blocks of 32 of them each.
-template <int DT_, int RT_, int NW_, int U_>
+// blocks of 32 of them each; P tiles are on their way while one is worked on.
+template <int DT_, int RT_, int NW_, int U_, int P_>
 struct Shape {
-    static constexpr int DT = DT_, RT = RT_, NW = NW_, U = U_;
+    static constexpr int DT = DT_, RT = RT_, NW = NW_, U = U_, P = P_;
     static constexpr int KW = NW / RT;               // waves to a row block
     static constexpr int KT = 32 * KW * U;           // entries of a tile
     static constexpr int ROWS = 32 * RT;
     static constexpr int NT = 64 * NW;
     static constexpr int KS = DT / 16, DB = DT / 32; // steps of QK, blocks of O's columns
-    // LDS rows: 16 bytes more than K's data spread a column's 16-byte reads over
-    // the banks, 64 more than V's the 4x16 blocks of the transposing reads
-    static constexpr int KROW = DT * 2 + 16, VROW = DT * 2 + 64;
-    static constexpr int CH = DT / 8;                // 16-byte vectors of a row
-    static constexpr int LOADS = KT * CH / NT;       // of K, and of V, a thread
-    static constexpr int LDS_KV = KT * (KROW + VROW);
-    static constexpr int LDS_OUT = KW > 1 ? (NW - RT) * 64 * DB * 16 * 4 : 0;
-    static constexpr int LDS = LDS_KV > LDS_OUT ? LDS_KV : LDS_OUT;
-    // a partial result: O^T as the lanes hold it, then maximum and sum of each row
-    static constexpr int PART = ROWS * DT + 2 * ROWS + 64;    // (and a flag)
-    static_assert(KT * CH % NT == 0 && NW % RT == 0, "shape");
+    static constexpr int ROWB = DT * 2;              // bytes of an LDS row
+    static constexpr int HALF = KT * ROWB;           // of a tile's K, and of its V
+    static constexpr int J = HALF / (NW * 1024);     // loads of 1024 bytes of each a wave
+    static constexpr int RPW = KT / NW;              // rows of each that a wave loads
+    static constexpr int RPL = 1024 / ROWB;          // rows of a load
+    static constexpr int RING = (P + 1) * 2 * HALF;
+    static constexpr int PAGES = P * NW * 64 * 4;    // page numbers on their way
+    static constexpr int LDS = RING + PAGES;
+    static constexpr int RESIDENT = LDS <= 79 * 1024 && NW <= 4 ? 2 : 1;   // workgroups a unit
+    static constexpr int WAVES = (RESIDENT * NW + 3) / 4;                  // waves a SIMD
+    // a partial result: O^T as the lanes hold it, maximum and sum of each row, a flag
+    static constexpr int PART = ROWS * DT + 2 * ROWS + 64;
+    static_assert(HALF % (NW * 1024) == 0 && NW % RT == 0 && RPW <= 64, "shape");
+    static_assert(KW == 1 || (NW - RT) * 64 * DB * 16 * 4 <= RING, "joining the waves in the ring");
+    static_assert((P - 1) * (2 * J + 1) < 64 && P * (2 * J + 1) < 64, "loads in flight");
 };
 
 struct AttnArgs {
@@ -183,6 +187,32 @@ __device__ __forceinline__ f32x16 mfma(const u32x4& a, const u32x4& b, const f32
                                                       __builtin_bit_cast(v8, b), c, 0, 0, 0);
 }
 
+// Loads from global memory straight into LDS, 16 or 4 bytes a lane, the lanes'
+// next to each other from `lds` on.  They are in flight until wait_loads; the
+// compiler does not know of them, which only makes its own waits longer.  (Its
+// builtin would make every LDS read wait for all of them.)  No register is
+// written.
+__device__ __forceinline__ void load_lds16(uint32_t lds, const void* p) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p)
+                 : "memory");
+}
+__device__ __forceinline__ void load_lds4(uint32_t lds, const void* p) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(p)
+                 : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// The 16-byte vectors of an LDS row lie in another order, so that reads of one
+// column hit different banks: vector c of row r at place c ^ k_turn(r) for K (16
+// rows, one vector each), c ^ v_turn(r) for V (4 rows, four vectors each).
+template <int DT>
+__device__ __forceinline__ int k_turn(int r) { return DT == 64 ? (r >> 1) & 7 : r & 15; }
+template <int DT>
+__device__ __forceinline__ int v_turn(int r) { return DT == 64 ? (r << 1) & 4 : (r << 2) & 12; }
+
 // A value of the lane's own and of the other half's lane of the same column.
 __device__ __forceinline__ f32x2 both_halves(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
@@ -245,12 +275,11 @@ struct Rows {
 }  // namespace
 
 template <typename T, typename S>
-__global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention(AttnArgs p) {
-    extern __shared__ __align__(16) char s_lds[];
+__global__ __launch_bounds__(S::NT) __attribute__((amdgpu_waves_per_eu(S::WAVES, S::WAVES))) void
+k_tree_attention(AttnArgs p) {
+    extern __shared__ __align__(1024) char s_lds[];
     __shared__ float s_ml[S::KW > 1 ? S::NW * 64 : 2];
     __shared__ int s_bad;                            // values left out of the item's products
-    char* const s_k = s_lds;
-    char* const s_v = s_lds + S::KT * S::KROW;
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int rt = wave % S::RT, kw = wave / S::RT;
@@ -258,6 +287,15 @@ __global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention
     const rheo_attention_args& a = p.a;
     const int w = blockIdx.x, D = c.D;
     const float to2 = a.scale * kLog2e;              // scores to exponents of 2
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_lds;
+    const uint32_t lds_mine = __builtin_amdgcn_readfirstlane(lds0 + wave * (S::J * 1024));
+    const uint32_t lds_pages = __builtin_amdgcn_readfirstlane(lds0 + S::RING + wave * 256);
+    const int* const pages = (const int*)(s_lds + S::RING + wave * 256);
+    // byte offsets in their rows of the lane's K vector for s = 0 and its part of a
+    // 4x16 block of V for d = 0 (others: exclusive or of 32 s, 64 d)
+    const int k_at = (half ^ k_turn<S::DT>(col)) * 16;
+    const int v_at = ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_turn<S::DT>((lane & 15) / 4)) * 16 +
+                     (lane & 1) * 8;
     if (tid == 0) s_bad = 0;
 
     const Stretch st = find_stretch<S>(p, w);
@@ -294,46 +332,41 @@ __global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention
         }
     }
 
-    uint4 kr[S::LOADS], vr[S::LOADS];
-    int pid[S::LOADS];
     for (bool first = true; left > 0; first = false) {
         const int tiles = tiles_of<S>(p, sq, rb);
         const int end_tile = (int)min((int64_t)tiles, tile + left);
         const int32_t* row_table = a.table + (int64_t)b * c.width;
-        const int64_t head = (int64_t)hk * D;
         const int entries = sq.entries, len = sq.len;
+        const T* const k_head = (const T*)a.k_cache + (int64_t)hk * D;
+        const T* const v_head = (const T*)a.v_cache + (int64_t)hk * D;
 
-        // the pages of a tile's entries, and the entries
+        // Tile t's page numbers, those of the rows that the wave loads; then its
+        // entries.  (Rows past the last entry and vectors past the head's last
+        // load the last one's again.)
         auto fetch_pages = [&](int t) {
+            const int e = t * S::KT + wave * S::RPW + min(lane, S::RPW - 1);
+            load_lds4(lds_pages + t % S::P * (S::NW * 256),
+                      row_table + (min(e, entries - 1) >> c.page_shift));
+        };
+        auto fetch = [&](int t) {
+            const uint32_t to = lds_mine + t % (S::P + 1) * (2 * S::HALF);
+            const int in_page = (1 << c.page_shift) - 1;
 #pragma unroll
-            for (int v = 0; v < S::LOADS; ++v) {
-                const int row = (tid + v * S::NT) / S::CH;
-                const int e = min(t * S::KT + row, entries - 1);
-                int page = entries > 0 ? row_table[e >> c.page_shift] : 0;
+            for (int j = 0; j < S::J; ++j) {
+                const int sub = j * S::RPL + lane * 16 / S::ROWB, row = wave * S::RPW + sub;
+                const int place = lane * 16 % S::ROWB / 16;
+                int page = pages[t % S::P * (S::NW * 64) + sub];
                 if ((unsigned)page >= (unsigned)c.pages) {
                     atomicOr(c.err, CE_PAGE);
                     page = 0;
                 }
-                pid[v] = page;
+                const int e = min(t * S::KT + row, entries - 1);
+                const int64_t at = page * c.page_stride + (e & in_page) * (c.K * D);
+                load_lds16(to + j * 1024, k_head + at + min(place ^ k_turn<S::DT>(row), D / 8 - 1) * 8);
+                load_lds16(to + S::HALF + j * 1024,
+                           v_head + at + min(place ^ v_turn<S::DT>(row), D / 8 - 1) * 8);
             }
         };
-        auto fetch = [&](int t) {
-            const bool part = (t + 1) * S::KT > entries || D < S::DT;
-#pragma unroll
-            for (int v = 0; v < S::LOADS; ++v) {
-                const int idx = tid + v * S::NT, row = idx / S::CH, ch = idx % S::CH;
-                int e = t * S::KT + row;
-                const bool in = e < entries && ch * 8 < D;
-                e = max(min(e, entries - 1), 0);
-                const int64_t at = pid[v] * c.page_stride +
-                                   (int64_t)(e & ((1 << c.page_shift) - 1)) * (c.K * D) + head +
-                                   min(ch * 8, D - 8);
-                kr[v] = *(const uint4*)((const T*)a.k_cache + at);
-                vr[v] = *(const uint4*)((const T*)a.v_cache + at);
-                if (part && !in) kr[v] = vr[v] = make_uint4(0, 0, 0, 0);
-            }
-        };
-
         Rows<S> x;
         const int r = rb * S::ROWS + rt * 32 + col;  // the lane's row of the item
         const bool live = r < sq.rows * p.g;
@@ -348,6 +381,24 @@ __global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention
                 if (live && d < D) x.q[s] = *(const u32x4*)(q + d);
             }
         }
+        __syncthreads();                             // the ring is free
+        if (entries > 0) {
+#pragma unroll
+            for (int i = 0; i < S::P; ++i)
+                if (tile + i < end_tile) fetch_pages(tile + i);
+        }
+        wait_loads<0>();
+        // (q is here, too: said so that no wait for it stands in the loop)
+#pragma unroll
+        for (int s = 0; s < S::KS; ++s) asm volatile("" : "+v"(x.q[s]));
+        if (entries > 0) {
+#pragma unroll
+            for (int i = 0; i < S::P; ++i) {
+                if (tile + i < end_tile) fetch(tile + i);
+                if (tile + i + S::P < end_tile) fetch_pages(tile + i + S::P);
+            }
+        }
+
 #pragma unroll
         for (int d = 0; d < S::DB; ++d) x.o[d] = 0.0f;
         x.m = -INFINITY;
@@ -355,36 +406,60 @@ __global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention
         const uint8_t* mrow = a.mask ? a.mask + qrow * a.tail : nullptr;
         const int reach = qi + a.tail - a.n;         // without a mask: tail entries seen, less 1
 
-        fetch_pages(tile);
-        fetch(tile);
-        if (tile + 1 < end_tile) fetch_pages(tile + 1);
-        for (int t = tile; t < end_tile; ++t) {
-            __syncthreads();                         // the tile before has been read
-            const bool tail_tile = (t + 1) * S::KT > len;
-#pragma unroll
-            for (int v = 0; v < S::LOADS; ++v) {
-                const int idx = tid + v * S::NT, row = idx / S::CH, ch = idx % S::CH;
-                *(uint4*)(s_k + row * S::KROW + ch * 16) = kr[v];
-                // An entry that some row does not attend must not reach it: 0 * inf
-                // is not 0.  Such values go in as zeros and are added at the end.
-                if (tail_tile && t * S::KT + row >= len && drop_unfinite<T>(vr[v])) s_bad = 1;
-                *(uint4*)(s_v + row * S::VROW + ch * 16) = vr[v];
+        for (int t = tile; t < end_tile && entries > 0; ++t) {
+            // Loads come in in order, so tile t's and the page numbers of tile t + P are
+            // there when no more are out than were sent after them
+            {
+                const int rd = min(S::P - 1, end_tile - 1 - t);
+                if (end_tile - 1 - t - S::P >= S::P - 1) wait_loads<(S::P - 1) * (2 * S::J + 1)>();
+                else if (S::P > 2 && rd == 2) wait_loads<(S::P > 2 ? 2 : 0) * 2 * S::J>();
+                else if (S::P > 1 && rd == 1) wait_loads<(S::P > 1 ? 1 : 0) * 2 * S::J>();
+                else wait_loads<0>();
             }
-            __syncthreads();
-            if (t + 1 < end_tile) fetch(t + 1);
-            if (t + 2 < end_tile) fetch_pages(t + 2);
+            char* const s_k = s_lds + t % (S::P + 1) * (2 * S::HALF);
+            char* const s_v = s_k + S::HALF;
+            const bool tail_tile = (t + 1) * S::KT > len;
+            if (tail_tile) {
+                // An entry that some row does not attend must not reach it: 0 * inf
+                // is not 0.  Such values become zeros and are added at the end.
+#pragma unroll
+                for (int j = 0; j < S::J; ++j) {
+                    const int e = t * S::KT + wave * S::RPW + j * S::RPL + lane * 16 / S::ROWB;
+                    if (e >= len) {
+                        uint4* v = (uint4*)(s_v + (wave * S::J + j) * 1024 + lane * 16);
+                        uint4 x = *v;
+                        const bool bad = drop_unfinite<T>(x);
+                        if (e >= entries) x = make_uint4(0, 0, 0, 0);
+                        else if (bad) s_bad = 1;
+                        *v = x;
+                    }
+                }
+            }
+            // (with one row block a wave works on the rows it has loaded itself)
+            if (S::RT > 1) __syncthreads();
+            if (t + S::P < end_tile) fetch(t + S::P);
+            if (t + 2 * S::P < end_tile) fetch_pages(t + 2 * S::P);
 
             // S^T of the wave's U blocks of 32 entries
             const int e0 = kw * S::U * 32;           // (of the tile)
             f32x16 sc[S::U];
 #pragma unroll
-            for (int u = 0; u < S::U; ++u) {
-                sc[u] = 0.0f;
-                const char* kp = s_k + (e0 + u * 32 + col) * S::KROW + half * 16;
+            for (int u = 0; u < S::U; ++u) sc[u] = 0.0f;
+            const char* const kp = s_k + (e0 + col) * S::ROWB;
 #pragma unroll
-                for (int s = 0; s < S::KS; ++s)
-                    sc[u] = mfma<T>(*(const u32x4*)(kp + s * 32), x.q[s], sc[u]);
+            for (int s = 0; s < S::KS; ++s)
+#pragma unroll
+                for (int u = 0; u < S::U; ++u)
+                    sc[u] = mfma<T>(*(const u32x4*)(kp + (k_at ^ s * 32) + u * 32 * S::ROWB), x.q[s],
+                                    sc[u]);
+            // six reads ahead of the products
+            __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+            for (int i = 0; i < S::KS * S::U - 6; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
+            __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
             if (tail_tile) {
                 const int eh = t * S::KT + e0 + 4 * half;
                 if (mrow && sq.tail > 0) {
@@ -445,17 +520,24 @@ __global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         pt[i] = pack2<T>(sc[u][8 * k + 2 * i], sc[u][8 * k + 2 * i + 1]);
-                    const char* vp = s_v + (e0 + u * 32 + 16 * k + 4 * half + (lane & 15) / 4) * S::VROW +
-                                     (16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
+                    const char* vp = s_v + (e0 + u * 32 + 16 * k + 4 * half + (lane & 15) / 4) * S::ROWB;
 #pragma unroll
                     for (int d = 0; d < S::DB; ++d) {
-                        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(vp + d * 64));
-                        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            (lds_s4)(vp + d * 64 + 8 * S::VROW));
+                        const char* vd = vp + (v_at ^ d * 64);
+                        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)vd);
+                        const s16x4 hi =
+                            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(vd + 8 * S::ROWB));
                         const s16x8 va = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
                         x.o[d] = mfma<T>(__builtin_bit_cast(u32x4, va), pt, x.o[d]);
                     }
                 }
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 1);
+#pragma unroll
+            for (int i = 0; i < S::DB * S::U * 2 - 4; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, 4, 1);
         }
 
         // the waves of a row block put together
@@ -550,46 +632,80 @@ __global__ __launch_bounds__(S::NT, (S::DT > 128 ? 1 : 2)) void k_tree_attention
 }
 
 // The partial results of one cut item added up: block x of a launch has the item
-// that begins at cut x's left (see k_tree_attention), block y its 32 rows and
-// 32 elements; a wave takes eight of these, in pairs of the lanes' halves.
+// that stretch x describes (see k_tree_attention), block y its 32 rows and 32
+// elements.  The waves take every eighth partial result each; one adds these
+// eight up.
+constexpr int NTJ = 512;
+
 template <typename T, typename S>
-__global__ __launch_bounds__(256) void k_attn_join(AttnArgs p) {
+__global__ __launch_bounds__(NTJ) void k_attn_join(AttnArgs p) {
+    constexpr int NWJ = NTJ / 64;
+    __shared__ float s_o[NWJ][16][64], s_m[NWJ][32], s_l[NWJ][32];
+    __shared__ int s_flag[NWJ];
     const int* desc = p.desc + 8 * blockIdx.x;
     const int n = desc[0];
     if (n == 0) return;
     const int slot0 = desc[1], b = desc[2], hk = desc[3], rb = desc[4];
-    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5, i = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5, wave = threadIdx.x >> 6;
     const int rt = blockIdx.y / S::DB, d = blockIdx.y % S::DB;
     const rheo_attention_args& a = p.a;
     const CacheDev& c = p.c;
     const Seq sq = seq_of<S>(p, b);
-    const int r = rb * S::ROWS + rt * 32 + col;
-    const int at = 32 * d + 8 * i + 4 * half;
-    if (r >= sq.rows * p.g || at >= c.D) return;
-    // (slot0 is the first stretch's, maybe its second; the others' first)
-    const int w0 = slot0 >> 1;
-    auto part = [&](int k) { return c.part + (int64_t)(k ? 2 * (w0 + k) : slot0) * S::PART; };
-    const int ml = S::ROWS * S::DT + (rt * 32 + col) * 2;
-    const int oi = ((rt * S::DB + d) * 16 + 4 * i) * 64 + lane;
+    const int rows = sq.rows * p.g;
+    if (rb * S::ROWS + rt * 32 >= rows || 32 * d >= c.D) return;
     const float to2 = a.scale * kLog2e;
-    float m = -INFINITY;
-    for (int k = 0; k < n; ++k) m = fmaxf(m, part(k)[ml]);
-    const float ref = m == -INFINITY ? 0.0f : m * to2;
-    float l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    // (slot0 is the first stretch's, maybe its second; the others' first)
+    const int w0 = slot0 >> 1, ml = S::ROWS * S::DT + (rt * 32 + col) * 2;
+    const int oi = (rt * S::DB + d) * 16 * 64 + lane;
+    float m = -INFINITY, l = 0.0f, o[16];
     int bad = 0;
-    for (int k = 0; k < n; ++k) {
-        const float* q = part(k);
-        bad |= ((const int*)q)[S::PART - 1];
-        const float f = __builtin_amdgcn_exp2f(__fmaf_rn(q[ml], to2, -ref));
-        l = __fmaf_rn(q[ml + 1], f, l);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = __fmaf_rn(q[oi + 64 * e], f, o[e]);
+    for (int e = 0; e < 16; ++e) o[e] = 0.0f;
+    for (int k = wave; k < n; k += NWJ) {
+        const float* q = c.part + (int64_t)(k ? 2 * (w0 + k) : slot0) * S::PART;
+        const float qm = q[ml], ql = q[ml + 1], top = fmaxf(m, qm);
+        const float ref = top == -INFINITY ? 0.0f : top * to2;
+        const float f = __builtin_amdgcn_exp2f(__fmaf_rn(m, to2, -ref));
+        const float g = __builtin_amdgcn_exp2f(__fmaf_rn(qm, to2, -ref));
+        bad |= ((const int*)q)[S::PART - 1];
+        m = top;
+        l = __fmaf_rn(ql, g, l * f);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = __fmaf_rn(q[oi + 64 * e], g, o[e] * f);
     }
+    const int waves = min(n, NWJ);
+    if (wave < waves) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s_o[wave][e][lane] = o[e];
+        if (!half) {
+            s_m[wave][col] = m;
+            s_l[wave][col] = l;
+        }
+        if (lane == 0) s_flag[wave] = bad;
+    }
+    __syncthreads();
+    // eight elements a wave's lanes: wave i has registers 4i .. 4i + 3 of each lane
+    if (wave >= 4) return;
+    const int r = rb * S::ROWS + rt * 32 + col, at = 32 * d + 8 * wave + 4 * half;
+    m = -INFINITY;
+    for (int k = 0; k < waves; ++k) m = fmaxf(m, s_m[k][col]);
+    const float ref = m == -INFINITY ? 0.0f : m * to2;
+    l = 0.0f;
+    bad = 0;
+    float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k = 0; k < waves; ++k) {
+        const float f = __builtin_amdgcn_exp2f(__fmaf_rn(s_m[k][col], to2, -ref));
+        l = __fmaf_rn(s_l[k][col], f, l);
+        bad |= s_flag[k];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = __fmaf_rn(s_o[k][4 * wave + e][lane], f, x[e]);
+    }
+    if (r >= rows || at >= c.D) return;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     const int qi = r / p.g, qh = hk * p.g + r - qi * p.g;
     const int64_t qrow = (int64_t)b * a.n + qi;
     T* out = (T*)a.out + qrow * a.out_stride + (int64_t)qh * c.D;
-    *(uint2*)(out + at) = make_uint2(pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv));
+    *(uint2*)(out + at) = make_uint2(pack2<T>(x[0] * inv, x[1] * inv), pack2<T>(x[2] * inv, x[3] * inv));
     if (a.lse && at == 0) a.lse[qrow * c.H + qh] = m * a.scale + logf(l);
     if (bad) add_unfinite<T>(p, b, hk, sq, qi, out, at, c.D);
 }
@@ -601,35 +717,29 @@ template <int DT>
 struct Shapes;
 template <>
 struct Shapes<64> {
-    typedef Shape<64, 1, 4, 1> R1;
-    typedef Shape<64, 2, 4, 1> R2;
-    typedef Shape<64, 4, 4, 2> R4;
-    typedef Shape<64, 8, 8, 2> R8;
+    typedef Shape<64, 1, 4, 1, 3> R1;
+    typedef Shape<64, 2, 4, 1, 3> R2;
+    typedef Shape<64, 4, 8, 1, 3> R4;
+    typedef Shape<64, 8, 8, 2, 3> R8;
 };
 template <>
 struct Shapes<128> {
-    typedef Shape<128, 1, 4, 1> R1;
-    typedef Shape<128, 2, 4, 1> R2;
-    typedef Shape<128, 4, 4, 2> R4;
-    typedef Shape<128, 8, 8, 2> R8;
+    typedef Shape<128, 1, 2, 1, 3> R1;
+    typedef Shape<128, 2, 4, 1, 3> R2;
+    typedef Shape<128, 4, 8, 1, 3> R4;
+    typedef Shape<128, 8, 8, 2, 3> R8;
 };
 template <>
 struct Shapes<256> {
-    typedef Shape<256, 1, 4, 1> R1;
-    typedef Shape<256, 2, 4, 1> R2;
-    typedef Shape<256, 4, 4, 1> R4;
+    typedef Shape<256, 1, 2, 1, 1> R1;
+    typedef Shape<256, 2, 2, 1, 3> R2;
+    typedef Shape<256, 4, 4, 1, 3> R4;
     typedef R4 R8;
 };
 
-// Workgroups a compute unit holds at once.
-template <typename S>
-constexpr int resident() {
-    return S::DT > 128 || S::NW > 4 ? 1 : 2;
-}
-
 template <typename S>
 size_t part_floats(int units) {
-    return (size_t)units * resident<S>() * 2 * S::PART;
+    return (size_t)units * S::RESIDENT * 2 * S::PART;
 }
 
 template <int DT>
@@ -645,14 +755,14 @@ size_t workspace(int units) {
 
 template <typename T, typename S>
 hipError_t start(AttnArgs p, hipStream_t s) {
-    static_assert(S::LDS <= 160 * 1024 - 4096, "LDS");
-    p.groups = p.c.slots * resident<S>();
+    static_assert(S::LDS <= 156 * 1024, "LDS");
+    p.groups = p.c.slots * S::RESIDENT;
     p.min_tiles = 1;
     const void* fn = (const void*)k_tree_attention<T, S>;
     hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
     if (e != hipSuccess) return e;
     k_tree_attention<T, S><<<p.groups, S::NT, S::LDS, s>>>(p);
-    k_attn_join<T, S><<<dim3(p.groups, S::RT * S::DB), 256, 0, s>>>(p);
+    k_attn_join<T, S><<<dim3(p.groups, S::RT * S::DB), NTJ, 0, s>>>(p);
     return hipGetLastError();
 }
 
