@@ -631,28 +631,31 @@ k_tree_attention(AttnArgs p) {
     }
 }
 
-// The partial results of one cut item added up: block x of a launch has the item
-// that stretch x describes (see k_tree_attention), block y its 32 rows and 32
-// elements.  The waves take every eighth partial result each; one adds these
-// eight up.
+// The partial results of one cut item added up: block y of a launch has the item
+// that stretch y describes (see k_tree_attention), block x its 32 rows and WD
+// blocks of 32 elements, one of them a wave.  (x runs first, so an item's blocks
+// spread over the chip's XCDs; with y first, items cut 32 times all fell to one:
+// 57 us instead of 13.)  8 / WD waves share the partial
+// results of each and are added up in turn.
 constexpr int NTJ = 512;
 
-template <typename T, typename S>
+template <typename T, typename S, int WD>
 __global__ __launch_bounds__(NTJ) void k_attn_join(AttnArgs p) {
-    constexpr int NWJ = NTJ / 64;
-    __shared__ float s_o[NWJ][16][64], s_m[NWJ][32], s_l[NWJ][32];
-    __shared__ int s_flag[NWJ];
-    const int* desc = p.desc + 8 * blockIdx.x;
+    constexpr int NS = NTJ / 64 / WD;
+    __shared__ float s_o[NS][WD][16][64], s_m[NS][32], s_l[NS][32];
+    __shared__ int s_flag[NS];
+    const int* desc = p.desc + 8 * blockIdx.y;
     const int n = desc[0];
     if (n == 0) return;
     const int slot0 = desc[1], b = desc[2], hk = desc[3], rb = desc[4];
-    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5, wave = threadIdx.x >> 6;
-    const int rt = blockIdx.y / S::DB, d = blockIdx.y % S::DB;
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const int wave = threadIdx.x >> 6, wd = wave % WD, part0 = wave / WD;
+    const int rt = blockIdx.x / (S::DB / WD), d0 = blockIdx.x % (S::DB / WD) * WD, d = d0 + wd;
     const rheo_attention_args& a = p.a;
     const CacheDev& c = p.c;
     const Seq sq = seq_of<S>(p, b);
     const int rows = sq.rows * p.g;
-    if (rb * S::ROWS + rt * 32 >= rows || 32 * d >= c.D) return;
+    if (rb * S::ROWS + rt * 32 >= rows || 32 * d0 >= c.D) return;
     const float to2 = a.scale * kLog2e;
     // (slot0 is the first stretch's, maybe its second; the others' first)
     const int w0 = slot0 >> 1, ml = S::ROWS * S::DT + (rt * 32 + col) * 2;
@@ -661,53 +664,75 @@ __global__ __launch_bounds__(NTJ) void k_attn_join(AttnArgs p) {
     int bad = 0;
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[e] = 0.0f;
-    for (int k = wave; k < n; k += NWJ) {
-        const float* q = c.part + (int64_t)(k ? 2 * (w0 + k) : slot0) * S::PART;
-        const float qm = q[ml], ql = q[ml + 1], top = fmaxf(m, qm);
-        const float ref = top == -INFINITY ? 0.0f : top * to2;
-        const float f = __builtin_amdgcn_exp2f(__fmaf_rn(m, to2, -ref));
-        const float g = __builtin_amdgcn_exp2f(__fmaf_rn(qm, to2, -ref));
-        bad |= ((const int*)q)[S::PART - 1];
-        m = top;
-        l = __fmaf_rn(ql, g, l * f);
+    const int last = n - 1;
+    for (int k = part0; k < n; k += 2 * NS) {
+        // two at a time (the second may be there twice, with weight 0)
+        const int k1 = min(k + NS, last);
+        const float* q0 = c.part + (int64_t)(k ? 2 * (w0 + k) : slot0) * S::PART;
+        const float* q1 = c.part + (int64_t)(k1 ? 2 * (w0 + k1) : slot0) * S::PART;
+        float x0[16], x1[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) o[e] = __fmaf_rn(q[oi + 64 * e], g, o[e] * f);
-    }
-    const int waves = min(n, NWJ);
-    if (wave < waves) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s_o[wave][e][lane] = o[e];
-        if (!half) {
-            s_m[wave][col] = m;
-            s_l[wave][col] = l;
+        for (int e = 0; e < 16; ++e) {
+            x0[e] = q0[oi + 64 * e];
+            x1[e] = q1[oi + 64 * e];
         }
-        if (lane == 0) s_flag[wave] = bad;
+        const float m0 = q0[ml], l0 = q0[ml + 1];
+        const float m1 = k + NS < n ? q1[ml] : -INFINITY, l1 = q1[ml + 1];
+        bad |= ((const int*)q0)[S::PART - 1] | ((const int*)q1)[S::PART - 1];
+        const float top = fmaxf(m, fmaxf(m0, m1)), ref = top == -INFINITY ? 0.0f : top * to2;
+        const float f = __builtin_amdgcn_exp2f(__fmaf_rn(m, to2, -ref));
+        const float g0 = __builtin_amdgcn_exp2f(__fmaf_rn(m0, to2, -ref));
+        const float g1 = __builtin_amdgcn_exp2f(__fmaf_rn(m1, to2, -ref));
+        m = top;
+        l = l * f + l0 * g0;
+        if (k + NS < n) l = __fmaf_rn(l1, g1, l);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            o[e] = __fmaf_rn(x0[e], g0, o[e] * f);
+            if (k + NS < n) o[e] = __fmaf_rn(x1[e], g1, o[e]);
+        }
+    }
+    if (part0 < n) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s_o[part0][wd][e][lane] = o[e];
+        if (wd == 0) {
+            if (!half) {
+                s_m[part0][col] = m;
+                s_l[part0][col] = l;
+            }
+            if (lane == 0) s_flag[part0] = bad;
+        }
     }
     __syncthreads();
-    // eight elements a wave's lanes: wave i has registers 4i .. 4i + 3 of each lane
-    if (wave >= 4) return;
-    const int r = rb * S::ROWS + rt * 32 + col, at = 32 * d + 8 * wave + 4 * half;
+    const int parts = min(n, NS), r = rb * S::ROWS + rt * 32 + col;
     m = -INFINITY;
-    for (int k = 0; k < waves; ++k) m = fmaxf(m, s_m[k][col]);
+    for (int k = 0; k < parts; ++k) m = fmaxf(m, s_m[k][col]);
     const float ref = m == -INFINITY ? 0.0f : m * to2;
     l = 0.0f;
     bad = 0;
-    float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k = 0; k < waves; ++k) {
-        const float f = __builtin_amdgcn_exp2f(__fmaf_rn(s_m[k][col], to2, -ref));
-        l = __fmaf_rn(s_l[k][col], f, l);
+    for (int k = 0; k < parts; ++k) {
+        l = __fmaf_rn(s_l[k][col], __builtin_amdgcn_exp2f(__fmaf_rn(s_m[k][col], to2, -ref)), l);
         bad |= s_flag[k];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = __fmaf_rn(s_o[k][4 * wave + e][lane], f, x[e]);
     }
-    if (r >= rows || at >= c.D) return;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     const int qi = r / p.g, qh = hk * p.g + r - qi * p.g;
     const int64_t qrow = (int64_t)b * a.n + qi;
     T* out = (T*)a.out + qrow * a.out_stride + (int64_t)qh * c.D;
-    *(uint2*)(out + at) = make_uint2(pack2<T>(x[0] * inv, x[1] * inv), pack2<T>(x[2] * inv, x[3] * inv));
-    if (a.lse && at == 0) a.lse[qrow * c.H + qh] = m * a.scale + logf(l);
-    if (bad) add_unfinite<T>(p, b, hk, sq, qi, out, at, c.D);
+    // four elements a lane and turn: registers 4i .. 4i + 3 of a block of 32
+    for (int f = wave; f < 4 * WD; f += NTJ / 64) {
+        const int i = f % 4, at = 32 * (d0 + f / 4) + 8 * i + 4 * half;
+        float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k = 0; k < parts; ++k) {
+            const float g = __builtin_amdgcn_exp2f(__fmaf_rn(s_m[k][col], to2, -ref));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = __fmaf_rn(s_o[k][f / 4][4 * i + e][lane], g, x[e]);
+        }
+        if (r >= rows || at >= c.D) continue;
+        *(uint2*)(out + at) =
+            make_uint2(pack2<T>(x[0] * inv, x[1] * inv), pack2<T>(x[2] * inv, x[3] * inv));
+        if (a.lse && at == 0) a.lse[qrow * c.H + qh] = m * a.scale + logf(l);
+        if (bad) add_unfinite<T>(p, b, hk, sq, qi, out, at, c.D);
+    }
 }
 
 namespace {
@@ -762,7 +787,14 @@ hipError_t start(AttnArgs p, hipStream_t s) {
     hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
     if (e != hipSuccess) return e;
     k_tree_attention<T, S><<<p.groups, S::NT, S::LDS, s>>>(p);
-    k_attn_join<T, S><<<dim3(p.groups, S::RT * S::DB), NTJ, 0, s>>>(p);
+    // Items that are cut once or twice take a wave a block of 32 elements, those of
+    // which many stretches have a part eight waves
+    constexpr int WD = S::DB < 4 ? S::DB : 4;
+    const int64_t items = (int64_t)p.c.B * p.c.K * (((int64_t)p.a.n * p.g + S::ROWS - 1) / S::ROWS);
+    if (items * 4 >= p.groups)
+        k_attn_join<T, S, WD><<<dim3(S::RT * (S::DB / WD), p.groups), NTJ, 0, s>>>(p);
+    else
+        k_attn_join<T, S, 1><<<dim3(S::RT * S::DB, p.groups), NTJ, 0, s>>>(p);
     return hipGetLastError();
 }
 
