@@ -36,13 +36,26 @@ __global__ __launch_bounds__(NTC) void k_cache_commit(CacheDev c, CommitArgs a, 
         bool good = took >= 0 && !bad;
         int node = 0;
         if (lane == 0) s_path[0] = 0;
+        // the first 128 nodes in registers: a level is then no memory's latency
+        int par[2], tok[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int i = min(64 * k + lane, a.n - 1);
+            par[k] = 64 * k + lane < a.n ? parent[i] : -2;
+            tok[k] = token[i];
+        }
         if (good) {
             const int want_lane = lane < took ? a.accepted[(int64_t)b * a.depth + lane] : -1;
             for (int j = 0; j < took && good; ++j) {
                 const int want = __shfl(want_lane, j);
                 int found = 0;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint64_t m = __ballot(par[k] == node && tok[k] == want);
+                    if (m && !found) found = 64 * k + __builtin_ctzll(m);
+                }
                 // (children come behind their parents, so the search starts there)
-                for (int i0 = node + 1; i0 < a.n && !found; i0 += 64) {
+                for (int i0 = max(node + 1, 128); i0 < a.n && !found; i0 += 64) {
                     const int i = i0 + lane;
                     const bool hit = i < a.n && parent[i] == node && token[i] == want;
                     const uint64_t m = __ballot(hit);
@@ -105,23 +118,27 @@ __global__ __launch_bounds__(NTC) void k_cache_commit(CacheDev c, CommitArgs a, 
             const int layer = f / (2 * vecs), g = f - layer * 2 * vecs;
             char* base = (g < vecs ? a.k_cache : a.v_cache) + layer * c.layer_stride * 2 +
                          (int64_t)(g < vecs ? g : g - vecs) * 16;
-            for (int j0 = 0; j0 < moves; j0 += 8) {
-                uint4 x[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    x[k] = *(const uint4*)(base + s_src[min(j0 + k, moves - 1)]);
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (j0 + k < moves) *(uint4*)(base + s_dst[j0 + k]) = x[k];
+            // four loads at a time (`moves` is the block's)
+            for (int j0 = 0; j0 < moves; j0 += 4) {
+                const int n = moves - j0;
+                uint4 x0 = *(const uint4*)(base + s_src[j0]), x1 = x0, x2 = x0, x3 = x0;
+                if (n > 1) x1 = *(const uint4*)(base + s_src[j0 + 1]);
+                if (n > 2) x2 = *(const uint4*)(base + s_src[j0 + 2]);
+                if (n > 3) x3 = *(const uint4*)(base + s_src[j0 + 3]);
+                *(uint4*)(base + s_dst[j0]) = x0;
+                if (n > 1) *(uint4*)(base + s_dst[j0 + 1]) = x1;
+                if (n > 2) *(uint4*)(base + s_dst[j0 + 2]) = x2;
+                if (n > 3) *(uint4*)(base + s_dst[j0 + 3]) = x3;
             }
         }
     }
     // new_lens may be lens itself: the sequence's last block writes it, when all
-    // have read theirs
+    // have read theirs.  (No data passes between the blocks, so the count needs no
+    // fence; one, which writes the L2 back, took 100 us at 2048 blocks.)
     __syncthreads();
     if (tid == 0) {
-        __threadfence();
-        if (split == 1 || atomicAdd(c.ticket + b, 1u) == (uint32_t)split - 1) {
+        if (split == 1 || __hip_atomic_fetch_add(c.ticket + b, 1u, __ATOMIC_RELAXED,
+                                                 __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)split - 1) {
             if (split > 1) c.ticket[b] = 0;
             a.new_lens[b] = s_len;
         }

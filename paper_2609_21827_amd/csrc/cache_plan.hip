@@ -39,21 +39,30 @@ __device__ __forceinline__ int clamp31(int64_t v) {
 // call is read from that sequence's row of the table, which nobody writes
 // there.  What the sums are taken from (held, free_count) is written by
 // the last block to finish, when all have read it.
+//
+// Latency is all there is (1 MB at 1024 sequences of 81 rows): the sums are one
+// round of loads and one exchange, and a block's rows are worked on all at once.
 __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
-    extern __shared__ int s_sum[];           // [B] pages lacked before, [B] returned before
+    // [B + 1] pages lacked by all before, [B + 1] returned; [B] pages needed (-1:
+    // out of range or too many)
+    extern __shared__ int s_sum[];
     __shared__ int64_t s_wave[2][NTP / 64];
     __shared__ int s_last;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int* s_take = s_sum;
-    int* s_give = s_sum + c.B;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, B = c.B;
+    int* const s_take = s_sum;
+    int* const s_give = s_take + B + 1;
+    int* const s_need = s_give + B + 1;
     // consecutive sequences a thread, then the threads' sums
-    const int per = (c.B + NTP - 1) / NTP, b0 = min(tid * per, c.B), b1 = min(b0 + per, c.B);
+    const int per = (B + NTP - 1) / NTP, b0 = min(tid * per, B), b1 = min(b0 + per, B);
+    const int have0 = *a.free_count;
     int64_t take = 0, give = 0;
     bool bad = false;
+#pragma unroll 4
     for (int b = b0; b < b1; ++b) {
         const Demand d = demand_of(c, a, b);
         s_take[b] = clamp31(take);           // (relative to the thread's first)
         s_give[b] = clamp31(give);
+        s_need[b] = d.fits ? d.need : -1;
         take += d.take;
         give += d.give;
         bad |= !d.valid;
@@ -65,21 +74,28 @@ __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
     }
     if (lane == 63) { s_wave[0][wave] = ti; s_wave[1][wave] = gi; }
     __syncthreads();
-    int64_t tb = ti - take, gb = gi - give, gives = 0;
+    int64_t tb = ti - take, gb = gi - give, takes = 0, gives = 0;
     for (int w = 0; w < NTP / 64; ++w) {
         if (w < wave) { tb += s_wave[0][w]; gb += s_wave[1][w]; }
+        takes += s_wave[0][w];
         gives += s_wave[1][w];
     }
     for (int b = b0; b < b1; ++b) {
         s_take[b] = clamp31(tb + s_take[b]);
         s_give[b] = clamp31(gb + s_give[b]);
     }
-    const int have0 = *a.free_count;
+    if (tid == 0) {
+        s_take[B] = clamp31(takes);
+        s_give[B] = clamp31(gives);
+    }
     const int have = min(max(have0, 0), c.pages);
     bad |= have != have0 || have + gives > c.pages;
     const int64_t room = have + gives;
     __syncthreads();
     if (blockIdx.x == 0 && bad) atomicOr(c.err, CE_PLAN);
+    auto served = [&](int b) {
+        return s_need[b] >= 0 && (s_take[b + 1] == s_take[b] || s_take[b + 1] <= room);
+    };
 
     // page number v of the stack after the pushes
     auto stack_page = [&](int64_t v) -> int {
@@ -87,16 +103,16 @@ __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
         if (v < have) {
             page = a.free_list[v];
         } else {
-            // the (room - 1 - v)-th returned page: the sequence it is of, then its place
+            // the (room - 1 - v)-th returned page: the last sequence that fewer are
+            // returned before (those that return none share their sum with the next)
             const int r = (int)(room - 1 - v);
-            int lo = 0, hi = c.B - 1;
+            int lo = 0, hi = B - 1;
             while (lo < hi) {
                 const int mid = (lo + hi + 1) >> 1;
                 if (s_give[mid] <= r) lo = mid; else hi = mid - 1;
             }
-            // (sequences that return nothing share their sum with the next)
-            const Demand d = demand_of(c, a, lo);
-            page = a.table[(int64_t)lo * c.width + min(d.need + r - s_give[lo], c.width - 1)];
+            page = a.table[(int64_t)lo * c.width +
+                           min(max(s_need[lo], 0) + r - s_give[lo], c.width - 1)];
         }
         if ((unsigned)page >= (unsigned)c.pages) {
             atomicOr(c.err, CE_PLAN);
@@ -105,72 +121,77 @@ __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
         return page;
     };
 
-    for (int b = blockIdx.x; b < c.B; b += gridDim.x) {
-        const Demand d = demand_of(c, a, b);
-        const int held = a.held[b], before = s_take[b];
-        const bool served = d.fits && (d.take == 0 || (int64_t)before + d.take <= room);
-        int32_t* row = a.table + (int64_t)b * c.width;
-        const int64_t top = room - 1 - before + held;    // (place p's page: stack_page(top - p))
-        if (served && d.take)
-            for (int p = held + tid; p < d.need; p += NTP) row[p] = stack_page(top - p);
-        const int len = a.lens[b];
-        const int count = !served ? 0 : a.count ? a.count[b] : a.n;
-        for (int i = tid; i < a.n; i += NTP) {
-            int64_t slot = -1;
-            int pos = -1;
-            if (i < count) {
-                const int e = len + i, p = e >> c.page_shift;
-                int page = p < held ? row[p] : stack_page(top - p);
-                if ((unsigned)page >= (unsigned)c.pages) {
-                    atomicOr(c.err, CE_PAGE);
-                } else {
-                    slot = ((int64_t)page << c.page_shift) + (e & ((1 << c.page_shift) - 1));
-                    pos = len + (a.depth ? a.depth[(int64_t)b * a.n + i] : i);
-                }
+    // the block's sequences: blockIdx.x and every gridDim.x-th after it, their new
+    // pages (16 threads each) and their rows all at once
+    const int mine = (B - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
+    for (int k = tid / 16; k < mine; k += NTP / 16) {
+        const int b = blockIdx.x + k * gridDim.x, took = s_take[b + 1] - s_take[b];
+        if (!served(b) || !took) continue;
+        const int held = s_need[b] - took;
+        for (int p = tid % 16; p < took; p += 16)
+            a.table[(int64_t)b * c.width + held + p] = stack_page(room - 1 - s_take[b] - p);
+    }
+    const int64_t rows = (int64_t)mine * a.n;
+    for (int64_t f = tid; f < rows; f += NTP) {
+        const int k = (int)(f / a.n), i = (int)(f - (int64_t)k * a.n);
+        const int b = blockIdx.x + k * gridDim.x;
+        const int64_t at = (int64_t)b * a.n + i;
+        const int len = a.lens[b], count = a.count ? a.count[b] : a.n;
+        const int depth = a.depth ? a.depth[at] : i;
+        int64_t slot = -1;
+        int pos = -1;
+        if (served(b) && i < count) {
+            const int held = s_need[b] - (s_take[b + 1] - s_take[b]);    // (or more)
+            const int e = len + i, p = e >> c.page_shift;
+            const int page = p < held ? a.table[(int64_t)b * c.width + p]
+                                      : stack_page(room - 1 - s_take[b] - (p - held));
+            if ((unsigned)page >= (unsigned)c.pages) {
+                atomicOr(c.err, CE_PAGE);
+            } else {
+                slot = ((int64_t)page << c.page_shift) + (e & ((1 << c.page_shift) - 1));
+                pos = len + depth;
             }
-            a.slots[(int64_t)b * a.n + i] = slot;
-            a.positions[(int64_t)b * a.n + i] = pos;
         }
-        if (tid == 0) a.status[b] = served ? 0 : d.fits ? 1 : 2;
+        a.slots[at] = slot;
+        a.positions[at] = pos;
+    }
+    for (int k = tid; k < mine; k += NTP) {
+        const int b = blockIdx.x + k * gridDim.x;
+        a.status[b] = served(b) ? 0 : s_need[b] >= 0 ? 1 : 2;
     }
 
-    // every read of this block is done
+    // every read of this block is done (no data passes to the last block, so the
+    // count needs no fence)
     __syncthreads();
     if (gridDim.x > 1) {
-        if (tid == 0) {
-            __threadfence();
-            s_last = atomicAdd(c.ticket + c.B, 1u) == gridDim.x - 1;
-        }
+        if (tid == 0)
+            s_last = __hip_atomic_fetch_add(c.ticket + B, 1u, __ATOMIC_RELAXED,
+                                            __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
         __syncthreads();
         if (!s_last) return;
-        if (tid == 0) c.ticket[c.B] = 0;
+        if (tid == 0) c.ticket[B] = 0;
     }
-    int64_t used = 0;
+    // pages popped: up to the last sequence that got any
+    int used = 0;
     for (int b = b0; b < b1; ++b) {
-        const Demand d = demand_of(c, a, b);
-        if (d.fits && d.take && (int64_t)s_take[b] + d.take <= room) used += d.take;
+        if (s_need[b] >= 0 && s_take[b + 1] > s_take[b] && s_take[b + 1] <= room)
+            used = s_take[b + 1];
+        if (served(b)) a.held[b] = s_need[b];
     }
-    for (int o = 32; o; o >>= 1) used += __shfl_xor(used, o);
-    __syncthreads();
+    for (int o = 32; o; o >>= 1) used = max(used, __shfl_xor(used, o));
     if (lane == 0) s_wave[0][wave] = used;
     __syncthreads();
-    used = 0;
-    for (int w = 0; w < NTP / 64; ++w) used += s_wave[0][w];
+    for (int w = 0; w < NTP / 64; ++w) used = max(used, (int)s_wave[0][w]);
     const int64_t left = room - used;
     // returned pages that were not popped again: only if fewer are left than
     // pushed, so that no block of this launch read the places written here
     for (int64_t v = have + tid; v < left && v < c.pages; v += NTP) a.free_list[v] = stack_page(v);
-    __syncthreads();
-    for (int b = b0; b < b1; ++b) {
-        const Demand d = demand_of(c, a, b);
-        if (d.fits && (d.take == 0 || (int64_t)s_take[b] + d.take <= room)) a.held[b] = d.need;
-    }
     if (tid == 0) *a.free_count = (int)min(left, (int64_t)c.pages);
 }
 
 hipError_t launch_cache_plan(const CacheDev& c, const PlanArgs& a, hipStream_t s) {
     const int blocks = c.B < 256 ? c.B : 256;
-    k_cache_plan<<<blocks, NTP, 2 * sizeof(int) * (size_t)c.B, s>>>(c, a);
+    k_cache_plan<<<blocks, NTP, sizeof(int) * (3 * (size_t)c.B + 2), s>>>(c, a);
     return hipGetLastError();
 }
 

@@ -87,26 +87,38 @@ __global__ __launch_bounds__(NTW) void k_cache_write(CacheDev c, rheo_write_args
     const int64_t entry = (slot >> c.page_shift) * c.page_stride +
                           (slot & place_mask) * ((int64_t)c.K * D);
     const int first = a.q ? 0 : c.H, heads = c.H + 2 * c.K;
-    for (int h = first + part * GROUPS + g; h < heads; h += parts * GROUPS) {
-        const T* src;
+    auto source = [&](int h) {
+        return h < c.H ? (const T*)a.q + (int64_t)row * a.q_stride + (int64_t)h * D
+               : h < c.H + c.K ? (const T*)a.k + (int64_t)row * a.k_stride + (int64_t)(h - c.H) * D
+                               : (const T*)a.v + (int64_t)row * a.v_stride + (int64_t)(h - c.H - c.K) * D;
+    };
+    int h = first + part * GROUPS + g;
+    uint4 na = {0, 0, 0, 0}, nb = {0, 0, 0, 0};      // the next head's vectors, on their way
+    if (h < heads) {
+        const T* src = source(h);
+        if (has_a) na = *(const uint4*)(src + 8 * va);
+        if (has_b) nb = *(const uint4*)(src + 8 * vb);
+    }
+    for (; h < heads; h += parts * GROUPS) {
+        const T* const src = source(h);
         T* dst;
         const T* w = nullptr;
         const bool value = h >= c.H + c.K;
         if (h < c.H) {
-            src = (const T*)a.q + (int64_t)row * a.q_stride + (int64_t)h * D;
             dst = (T*)a.q_out + (int64_t)row * a.q_out_stride + (int64_t)h * D;
             w = (const T*)a.q_weight;
         } else if (!value) {
-            src = (const T*)a.k + (int64_t)row * a.k_stride + (int64_t)(h - c.H) * D;
             dst = (T*)a.k_cache + entry + (int64_t)(h - c.H) * D;
             w = (const T*)a.k_weight;
         } else {
-            src = (const T*)a.v + (int64_t)row * a.v_stride + (int64_t)(h - c.H - c.K) * D;
             dst = (T*)a.v_cache + entry + (int64_t)(h - c.H - c.K) * D;
         }
-        const uint4 zero = make_uint4(0, 0, 0, 0);
-        uint4 xa = has_a ? *(const uint4*)(src + 8 * va) : zero;
-        uint4 xb = has_b ? *(const uint4*)(src + 8 * vb) : zero;
+        uint4 xa = na, xb = nb;
+        if (h + parts * GROUPS < heads) {
+            const T* s1 = source(h + parts * GROUPS);
+            if (has_a) na = *(const uint4*)(s1 + 8 * va);
+            if (has_b) nb = *(const uint4*)(s1 + 8 * vb);
+        }
         if (!value) {
             float x[16];
             unpack8<T>(xa, x);
@@ -136,8 +148,11 @@ __global__ __launch_bounds__(NTW) void k_cache_write(CacheDev c, rheo_write_args
             }
             if (w) {
                 float wf[16];
-                unpack8<T>(has_a ? *(const uint4*)(w + 8 * va) : zero, wf);
-                unpack8<T>(has_b ? *(const uint4*)(w + 8 * vb) : zero, wf + 8);
+                uint4 wa = {0, 0, 0, 0}, wb = {0, 0, 0, 0};
+                if (has_a) wa = *(const uint4*)(w + 8 * va);
+                if (has_b) wb = *(const uint4*)(w + 8 * vb);
+                unpack8<T>(wa, wf);
+                unpack8<T>(wb, wf + 8);
 #pragma unroll
                 for (int j = 0; j < 16; ++j) x[j] = x[j] * inv * wf[j];
             }
@@ -200,10 +215,10 @@ hipError_t launch_cache_write(const CacheDev& c, const rheo_write_args& a, hipSt
     // vectors, none more (rot_dim % 16 == 0 leaves (D - rot) / 8 vectors in pairs)
     const int lph = c.D <= 64 ? 4 : c.D <= 128 ? 8 : 16;
     const int heads = (a.q ? c.H : 0) + 2 * c.K, rounds = (heads + 64 / lph - 1) / (64 / lph);
-    // A wave takes all heads of a row while that leaves 16 waves to each of 256 compute
-    // units, and fewer heads of it below that, where latency counts
-    int parts = 4096 / (rows ? rows : 1);
-    parts = parts < 1 ? 1 : parts > rounds ? rounds : parts;
+    // A wave takes four rounds of a row's heads, and fewer where that leaves less
+    // than 16 waves to each of 256 compute units and latency counts
+    int parts = (rounds + 3) / 4;
+    if ((int64_t)rows * parts < 4096) parts = 4096 / rows < rounds ? 4096 / rows : rounds;
     const int64_t waves = (int64_t)rows * parts;
     const int blocks = (int)((waves + NTW / 64 - 1) / (NTW / 64));
     if (c.dtype == RHEO_BF16) start_lph<__bf16>(c, a, blocks, rows, parts, lph, s);

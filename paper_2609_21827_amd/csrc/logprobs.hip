@@ -17,7 +17,7 @@ constexpr int EPT = 16;                   // elements a thread holds of a chunk
 constexpr int CHUNK = NTL * EPT;          // 8192 elements
 constexpr int TOP = 32;                   // most alternatives
 constexpr int LIST = 1024;                // most candidates of a chunk
-constexpr int PARTS = 2048;               // most segments of a launch that splits rows
+constexpr int PARTS = 1024;               // most segments of a launch that splits rows
 constexpr float kLn2 = 0.69314718055994531f;
 
 // What a row, or a part of it, comes to: the largest logit, and with t = (l -
@@ -39,23 +39,34 @@ template <int DT>
 using Elem = typename std::conditional<DT == RHEO_F32, float,
              typename std::conditional<DT == RHEO_BF16, __bf16, _Float16>::type>::type;
 
-// The 16-byte vector at element e of a row as floats; past V -inf, which adds
-// nothing to a sum and orders behind every token by its id.
+// The 16-byte vector at element e of a row; past V -inf, which adds nothing to
+// a sum and orders behind every token by its id.
 template <int DT>
-__device__ __forceinline__ void load_vec(const char* row, int64_t e, int V, float* x) {
+__device__ __forceinline__ uint4 load_vec(const char* row, int64_t e, int V) {
     constexpr int VEC = DT == RHEO_F32 ? 4 : 8;
-    if (e + VEC <= V) {
-        const uint4 w = *(const uint4*)(row + e * sizeof(Elem<DT>));
-        if constexpr (DT == RHEO_F32) {
-            x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y);
-            x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
-        } else {
-            unpack8<Elem<DT>>(w, x);
-        }
-    } else {
+    if (e + VEC <= V) return *(const uint4*)(row + e * sizeof(Elem<DT>));
+    uint32_t w[4];
+    if constexpr (DT == RHEO_F32) {
 #pragma unroll
-        for (int k = 0; k < VEC; ++k)
-            x[k] = e + k < V ? (float)((const Elem<DT>*)row)[e + k] : -INFINITY;
+        for (int k = 0; k < 4; ++k) w[k] = e + k < V ? ((const uint32_t*)row)[e + k] : 0xFF800000u;
+    } else {
+        constexpr uint32_t low = DT == RHEO_BF16 ? 0xFF80u : 0xFC00u;
+        const uint16_t* h = (const uint16_t*)row;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            w[k] = (e + 2 * k < V ? h[e + 2 * k] : low) |
+                   (e + 2 * k + 1 < V ? h[e + 2 * k + 1] : low) << 16;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <int DT>
+__device__ __forceinline__ void unpack_vec(const uint4& v, float* x) {
+    if constexpr (DT == RHEO_F32) {
+        x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y);
+        x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+    } else {
+        unpack8<Elem<DT>>(v, x);
     }
 }
 
@@ -85,12 +96,12 @@ __device__ __forceinline__ Stat wave_join(Stat v, float kT) {
     return v;
 }
 
-// The k-th largest of a wave's 64 values (1 <= k <= 64): bit by bit from the
-// top, set where k values are at least that large.
+// A lower bound of the k-th largest of a wave's 64 values (1 <= k <= 64): its
+// upper 16 bits, from the top, each set where k values are at least that large.
 __device__ __forceinline__ uint32_t wave_kth(uint32_t v, int k) {
     uint32_t t = 0;
 #pragma unroll
-    for (int bit = 31; bit >= 0; --bit) {
+    for (int bit = 31; bit >= 16; --bit) {
         const uint32_t u = t | (1u << bit);
         if (__builtin_popcountll(__ballot(v >= u)) >= k) t = u;
     }
@@ -128,20 +139,27 @@ __device__ __forceinline__ void put_outputs(const LogprobArgs& a, int entry, con
 }  // namespace
 
 // One block takes a segment of one entry's row, chunk by chunk, every element
-// once from memory into a register: running maximum and sums a thread, the
-// tokens before the given one, and the best `top` keys so far in LDS (a key:
-// logit descending, id ascending, as one 64-bit number).
+// once from memory into a register, the next chunk on its way: running maximum
+// and sums a thread, the tokens before the given one, and a list in LDS of the
+// keys that may be among the best `top` (a key: logit descending, id ascending,
+// as one 64-bit number).
 //
-// Candidates of a chunk are the elements above a bound: the worst of the best
-// so far, or until there are `top` of them the largest of the waves' top-th
-// largest thread maxima (at least `top` elements of the chunk are that large).
-// They are ranked by counting.  Where more than LIST pass the bound (ties, rows
-// that rise), the chunk's top-th largest key is found bit by bit over the
-// registers: at most `top` are that large.
+// The list takes every element above a bound and is ranked, by counting, after
+// the first chunk, when it has twice `top` and 16, and at the end; the worst of the
+// best is then the bound.  The
+// first bound comes from the first chunk's thread maxima: with NWL waves, at least
+// `top` of its elements are as large as the least of the waves' ceil(top /
+// NWL)-th largest (of a chunk that leaves waves empty, as the largest of the
+// waves' top-th largest).  A chunk that overflows the list (ties, rows that
+// rise) is looked at again with its top-th largest key, found bit by bit over
+// the registers: at most `top` are that large.
+//
+// Bound by the row's bytes: 128 x 5 rows of 151936 bf16, 4 to 5 of 9 there
+// (MEASURED_HERE).
 template <int DT>
 __global__ __launch_bounds__(NTL) void k_row_stats(ScoreDev c, LogprobArgs a, int segs,
                                                    int seg_chunks) {
-    __shared__ uint64_t s_list[LIST + TOP], s_best[TOP];
+    __shared__ uint64_t s_list[LIST], s_best[TOP];
     __shared__ Stat s_stat[NWL];
     __shared__ int s_sum[NWL], s_cnt;
     __shared__ uint32_t s_bound[NWL];
@@ -155,17 +173,46 @@ __global__ __launch_bounds__(NTL) void k_row_stats(ScoreDev c, LogprobArgs a, in
     const char* row = a.logits + ((int64_t)b * a.n + line) * c.stride * sizeof(Elem<DT>);
     const int V = c.V, top = a.top;
     const float kT = a.kT;
-    const float lt = (float)((const Elem<DT>*)row)[token];
-    const uint64_t own = logit_key(lt, (uint32_t)token);
     const int first = seg * seg_chunks * CHUNK;
     const int end = min(V, first + seg_chunks * CHUNK);
+    uint4 next[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) next[v] = load_vec<DT>(row, first + (v * NTL + tid) * VEC, V);
+    const float lt = (float)((const Elem<DT>*)row)[token];
+    if (tid == 0) s_cnt = 0;
+    __syncthreads();
 
     Stat st = {-INFINITY, 0.0f, 0.0f, 0};
-    int best = 0;                          // keys in s_best
+    int listed = 0;                        // keys in s_list
+    uint64_t over = 0;                     // keys above it go in,
+    float low = 0.0f;                      // of logits at least that large
+    // the best of the list, sorted, at its front; `over` and `low` after them
+    auto rank = [&]() {
+        for (int i = tid; i < listed; i += NTL) {
+            const uint64_t key = s_list[i];
+            int r = 0;
+#pragma unroll 8
+            for (int j = 0; j < listed; ++j) r += s_list[j] > key;
+            if (r < top) s_best[r] = key;
+        }
+        listed = min(listed, top);
+        __syncthreads();
+        if (tid < listed) s_list[tid] = s_best[tid];
+        if (tid == 0) s_cnt = listed;
+        if (listed == top) {
+            over = s_best[top - 1];
+            low = key_value(over);
+        }
+        __syncthreads();
+    };
     for (int c0 = first; c0 < end; c0 += CHUNK) {
         float x[EPT];
 #pragma unroll
-        for (int v = 0; v < NV; ++v) load_vec<DT>(row, c0 + (v * NTL + tid) * VEC, V, x + v * VEC);
+        for (int v = 0; v < NV; ++v) unpack_vec<DT>(next[v], x + v * VEC);
+        if (c0 + CHUNK < end)
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+                next[v] = load_vec<DT>(row, c0 + CHUNK + (v * NTL + tid) * VEC, V);
         auto id_of = [&](int k) { return c0 + ((k / VEC) * NTL + tid) * VEC + k % VEC; };
 
         float m = x[0];
@@ -180,75 +227,78 @@ __global__ __launch_bounds__(NTL) void k_row_stats(ScoreDev c, LogprobArgs a, in
             const float e = __builtin_amdgcn_exp2f(t);
             st.s += e;
             st.st = __fmaf_rn(t, e, st.st);
-            st.before += logit_key(x[k], (uint32_t)id_of(k)) > own && id_of(k) < V;
+        }
+        // a tie goes before the token where its id is lower
+        if (c0 + CHUNK <= token) {
+#pragma unroll
+            for (int k = 0; k < EPT; ++k) st.before += x[k] >= lt;
+        } else if (c0 > token) {
+#pragma unroll
+            for (int k = 0; k < EPT; ++k) st.before += (x[k] > lt) & (id_of(k) < V);
+        } else {
+#pragma unroll
+            for (int k = 0; k < EPT; ++k)
+                st.before += (x[k] > lt) | ((x[k] == lt) & (id_of(k) < token));
         }
         if (top == 0) continue;
 
-        // the bound: codes at least `code` pass, and keys above `over`
-        uint64_t over = 0;
-        uint32_t code = 0;
-        const int left = min(V - c0, CHUNK);             // elements of the chunk
-        if (best == top) {
-            over = s_best[top - 1];
-            code = (uint32_t)(over >> 32);
-        } else {
-            const uint32_t kth = wave_kth(ord32(m), top);
+        if (c0 == first) {
+            const bool full = min(V - c0, CHUNK) >= NTL * VEC;
+            const uint32_t kth = wave_kth(ord32(m), full ? (top + NWL - 1) / NWL : top);
             if (lane == 0) s_bound[wave] = kth;
             __syncthreads();
+            uint32_t code = s_bound[0];
 #pragma unroll
-            for (int w = 0; w < NWL; ++w) code = max(code, s_bound[w]);
+            for (int w = 1; w < NWL; ++w)
+                code = full ? min(code, s_bound[w]) : max(code, s_bound[w]);
+            // (no NaN: the code is at least that of -inf, cut to its upper half)
+            low = code <= 0x007FFFFFu ? -INFINITY : unord32(code);
         }
-        int mine = 0;
-        const float low = unord32(code);                 // (no NaN: a logit's code, or 0)
-        if (code == 0 || m >= low) {
+        auto list = [&](int k) {
+            const uint64_t key = logit_key(x[k], (uint32_t)id_of(k));
+            if (key > over && id_of(k) < V) {
+                const int at = atomicAdd(&s_cnt, 1);
+                if (at < LIST) s_list[at] = key;
+            }
+        };
+        // (few threads have one: a branch an element, skipped by whole waves)
+        if (m >= low)
 #pragma unroll
             for (int k = 0; k < EPT; ++k)
-                mine += id_of(k) < V && ord32(x[k]) >= code && logit_key(x[k], id_of(k)) > over;
-        }
-        int total = block_count(mine, s_sum);
-        if (total > LIST) {
-            // the top-th largest key above `over`; 64 bits of it, since keys differ
-            const int k_th = min(top, left);
-            uint64_t t = 0;
-            for (int bit = 63; bit >= 0; --bit) {
-                const uint64_t u = t | (1ull << bit);
-                int cnt = 0;
-#pragma unroll
-                for (int k = 0; k < EPT; ++k)
-                    cnt += id_of(k) < V && logit_key(x[k], id_of(k)) >= u;
-                if (block_count(cnt, s_sum) >= k_th) t = u;
-            }
-            over = max(over, t - 1);
-            code = (uint32_t)(t >> 32);
-            mine = 0;
-#pragma unroll
-            for (int k = 0; k < EPT; ++k) mine += id_of(k) < V && logit_key(x[k], id_of(k)) > over;
-            total = block_count(mine, s_sum);
-        }
-        if (total == 0) continue;
-        // the candidates behind the best so far, in any order
-        if (tid == 0) s_cnt = best;
-        if (tid < best) s_list[tid] = s_best[tid];
+                if (x[k] >= low) list(k);
         __syncthreads();
-        if (mine) {
-            int at = atomicAdd(&s_cnt, mine);
+        const int total = s_cnt;
+        if (total <= LIST) {
+            listed = total;
+            if (c0 == first || total > 2 * top + 16) rank();
+            else __syncthreads();          // (s_cnt has been read)
+            continue;
+        }
+        // this chunk's keys are not all in: without them, then its best alone
+        __syncthreads();
+        rank();
+        const int k_th = min(top, min(V - c0, CHUNK));
+        uint64_t t = 0;
+        for (int bit = 63; bit >= 0; --bit) {
+            const uint64_t u = t | (1ull << bit);
+            int cnt = 0;
 #pragma unroll
-            for (int k = 0; k < EPT; ++k) {
-                const uint64_t key = logit_key(x[k], id_of(k));
-                if (id_of(k) < V && ord32(x[k]) >= code && key > over) s_list[at++] = key;
-            }
+            for (int k = 0; k < EPT; ++k)
+                cnt += id_of(k) < V && logit_key(x[k], (uint32_t)id_of(k)) >= u;
+            if (block_count(cnt, s_sum) >= k_th) t = u;
         }
+        if (t - 1 > over) over = t - 1;
+        low = fmaxf(low, key_value(t));
+#pragma unroll
+        for (int k = 0; k < EPT; ++k)
+            if (x[k] >= low) list(k);
         __syncthreads();
-        const int all = best + total;
-        for (int i = tid; i < all; i += NTL) {
-            const uint64_t key = s_list[i];
-            int rank = 0;
-            for (int j = 0; j < all; ++j) rank += s_list[j] > key;
-            if (rank < top) s_best[rank] = key;
-        }
-        best = min(all, top);
+        listed = s_cnt;
         __syncthreads();
+        rank();
     }
+    if (top) rank();
+    const int best = listed;
 
     st = wave_join(st, kT);
     if (lane == 0) s_stat[wave] = st;
