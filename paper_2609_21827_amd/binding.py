@@ -135,6 +135,14 @@ def _stream(stream):
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+def _current_stream(index):
+    """The address of torch's current stream on a device."""
+    return _RAW_STREAM(index) if _RAW_STREAM else torch.cuda.current_stream(index).cuda_stream
+
+
+_RAW_STREAM = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 class _CudaArray:
     """A device int32 array exposed through __cuda_array_interface__."""
 
@@ -276,34 +284,47 @@ def _refuse(msg):
 class _OnDevice:
     """What the handles below share: tensors are checked for place, type, shape and
     layout (nothing is copied or converted), outputs are allocated on the handle's
-    device, and a stream given by the caller is noted with the allocator."""
+    device, and a stream given by the caller is noted with the allocator.
 
-    def _device_of(self, device):
+    A call is some 5 us of checks and marshalling beside kernels of 4 us, so the
+    checks are few and plain: get_device() and `is` instead of device and dtype
+    objects compared, addresses as plain numbers."""
+
+    def _set_device(self, device):
         device = torch.device(device)
         if device.type != "cuda":
             _refuse(f"device must be a GPU, got {device}")
-        return torch.device("cuda", torch.cuda.current_device() if device.index is None
-                            else device.index)
+        self._index = torch.cuda.current_device() if device.index is None else device.index
+        self.device = torch.device("cuda", self._index)
 
     def _dense(self, t, dtype, shape, name):
-        """A contiguous tensor of exactly this type and shape."""
+        """The address of a contiguous tensor of exactly this type and shape."""
         if not isinstance(t, torch.Tensor):
             _refuse(f"{name} must be a tensor, got {type(t).__name__}")
-        if t.device != self.device or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index:
             _refuse(f"{name} must be {dtype} {tuple(shape)} on {self.device}, got {t.dtype} "
                     f"{tuple(t.shape)} on {t.device}")
         if not t.is_contiguous():
             _refuse(f"{name} must be contiguous")
-        return t
+        return t.data_ptr()
 
-    def _launch(self, stream, tensors, call):
-        """``call`` with the stream, noted for every tensor if it is not torch's own."""
-        own = torch.cuda.current_stream(self.device)
-        if stream is not None and stream != own:
+    def _made(self, t, dtype, shape, name):
+        """(tensor, address) of an output, allocated unless given."""
+        if t is None:
+            t = torch.empty(shape, dtype=dtype, device=self.device)
+            return t, t.data_ptr()
+        return t, self._dense(t, dtype, shape, name)
+
+    def _stream(self, stream, tensors):
+        """The stream to launch on; one that is not torch's current is noted for the
+        tensors, so that their memory is not used again before its work has run."""
+        if stream is None:
+            return _current_stream(self._index)
+        if stream.cuda_stream != _current_stream(self._index):
             for t in tensors:
                 if t is not None:
                     t.record_stream(stream)
-        _check(call(ctypes.c_void_p((stream or own).cuda_stream)))
+        return stream.cuda_stream
 
     def _open(self, create):
         h = ctypes.c_void_p()
@@ -338,7 +359,7 @@ class Cache(_OnDevice):
         lib = load_library()
         cfg = CacheConfig(batch, heads, kv_heads, head_dim, page_size, pages, table_width, layers,
                           _dtype_code(dtype), page_stride, layer_stride)
-        self.device = self._device_of(device)
+        self._set_device(device)
         self._destroy = lib.rheo_cache_destroy
         self._open(lambda h: lib.rheo_cache_create(ctypes.byref(cfg), h))
         self.B, self.H, self.K, self.D = batch, heads, kv_heads, head_dim
@@ -346,57 +367,54 @@ class Cache(_OnDevice):
         self.layers, self.dtype = layers, dtype
         self.page_stride = page_stride or page_size * kv_heads * head_dim
         self.layer_stride = layer_stride or pages * self.page_stride
+        self._page_shape = (pages, page_size, kv_heads, head_dim)
+        self._page_strides = (self.page_stride, kv_heads * head_dim, head_dim, 1)
 
     def _i32(self, t, shape, name):
         return None if t is None else self._dense(t, torch.int32, shape, name)
 
-    def _out(self, t, dtype, shape, name):
-        if t is None:
-            return torch.empty(shape, dtype=dtype, device=self.device)
-        return self._dense(t, dtype, shape, name)
-
     def _rows(self, t, n, heads, name):
-        """[B, n, heads, head_dim] with dense heads; returns the stride of a row."""
-        shape = (self.B, n, heads, self.D)
-        if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != self.dtype \
-                or tuple(t.shape) != shape:
+        """(address, elements between rows) of [B, n, heads, head_dim] with dense heads."""
+        B, D, shape = self.B, self.D, (self.B, n, heads, self.D)
+        if not isinstance(t, torch.Tensor) or t.dtype is not self.dtype or t.shape != shape \
+                or t.get_device() != self._index:
             _refuse(f"{name} must be {self.dtype} {shape} on {self.device}")
-        row = t.stride(1) if n > 1 else t.stride(0) if self.B > 1 else heads * self.D
-        if t.numel() and ((self.D > 1 and t.stride(3) != 1) or (heads > 1 and t.stride(2) != self.D)
-                          or (self.B > 1 and t.stride(0) != n * row) or row < heads * self.D):
+        s0, s1, s2, s3 = t.stride()
+        row = s1 if n > 1 else s0 if B > 1 else heads * D
+        if n and (s3 != 1 or (heads > 1 and s2 != D) or (B > 1 and s0 != n * row)
+                  or row < heads * D):
             _refuse(f"{name}: a row's heads must be dense and rows evenly apart over the batch")
-        return row
+        return t.data_ptr(), row
 
     def _pages(self, t, name, layers=None):
-        lead = () if layers is None else (layers,)
-        shape = lead + (self.pages, self.page_size, self.K, self.D)
-        if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != self.dtype \
-                or tuple(t.shape) != shape:
+        shape, want = self._page_shape, self._page_strides
+        if layers is not None:
+            shape, want = (layers,) + shape, (self.layer_stride,) + want
+        if not isinstance(t, torch.Tensor) or t.dtype is not self.dtype or t.shape != shape \
+                or t.get_device() != self._index:
             _refuse(f"{name} must be {self.dtype} {shape} on {self.device}")
-        want = (self.layer_stride,) if layers is not None else ()
-        want += (self.page_stride, self.K * self.D, self.D, 1)
-        if any(s != w for s, w, k in zip(t.stride(), want, shape) if k > 1):
+        if t.stride() != want and any(s != w for s, w, k in zip(t.stride(), want, shape) if k > 1):
             _refuse(f"{name} must have strides {want}, got {t.stride()}")
-        return t
+        return t.data_ptr()
 
     def plan(self, lens, held, table, free_list, free_count, n, count=None, depth=None, out=None,
              stream=None):
         """Pages and slots for the next n rows of each sequence; (slots [B, n] int64,
         positions [B, n] int32, status [B] int32).  held, table, free_list and
         free_count are updated in place."""
-        B = self.B
-        self._i32(lens, (B,), "lens"), self._i32(held, (B,), "held")
-        self._i32(table, (B, self.width), "table")
-        self._i32(free_list, (self.pages,), "free_list")
-        self._i32(free_count, (1,), "free_count")
-        self._i32(count, (B,), "count"), self._i32(depth, (B, n), "depth")
+        B, i32 = self.B, self._i32
+        one, rows = (B,), (B, n)
         slots, positions, status = out or (None, None, None)
-        slots = self._out(slots, torch.int64, (B, n), "slots")
-        positions = self._out(positions, torch.int32, (B, n), "positions")
-        status = self._out(status, torch.int32, (B,), "status")
-        ts = (lens, count, depth, held, table, free_list, free_count, slots, positions, status)
-        self._launch(stream, ts, lambda s: _LIB.rheo_cache_plan(
-            self._h, n, *[_ptr(t) for t in ts], s))
+        slots, p_slots = self._made(slots, torch.int64, rows, "slots")
+        positions, p_positions = self._made(positions, torch.int32, rows, "positions")
+        status, p_status = self._made(status, torch.int32, one, "status")
+        _check(_LIB.rheo_cache_plan(
+            self._h, n, i32(lens, one, "lens"), i32(count, one, "count"), i32(depth, rows, "depth"),
+            i32(held, one, "held"), i32(table, (B, self.width), "table"),
+            i32(free_list, (self.pages,), "free_list"), i32(free_count, (1,), "free_count"),
+            p_slots, p_positions, p_status,
+            self._stream(stream, (lens, count, depth, held, table, free_list, free_count, slots,
+                                  positions, status))))
         return slots, positions, status
 
     def write(self, q, k, v, slots, k_cache, v_cache, positions=None, rotation=None,
@@ -404,35 +422,37 @@ class Cache(_OnDevice):
         """Head norms (where a weight is given), rotation (where a table is: [max_position,
         rot_dim] float32, cosines then sines) and store; returns the rotated q
         (``out``, which may be q itself), or None if q is None."""
-        B, n = self.B, k.shape[1]
-        a = WriteArgs(n=n, interleaved=int(interleaved), eps=float(eps))
-        a.k_stride, a.v_stride = self._rows(k, n, self.K, "k"), self._rows(v, n, self.K, "v")
+        B, n, dim = self.B, k.shape[1], (self.D,)
+        p_k, k_row = self._rows(k, n, self.K, "k")
+        p_v, v_row = self._rows(v, n, self.K, "v")
+        p_q = p_out = q_row = out_row = 0
         if q is not None:
-            a.q_stride = self._rows(q, n, self.H, "q")
+            p_q, q_row = self._rows(q, n, self.H, "q")
             if out is None:
                 out = torch.empty((B, n, self.H, self.D), dtype=self.dtype, device=self.device)
-            a.q_out_stride = self._rows(out, n, self.H, "out")
+            p_out, out_row = self._rows(out, n, self.H, "out")
         elif out is not None:
             _refuse("out without q")
-        self._dense(slots, torch.int64, (B, n), "slots")
+        rot_dim = most = 0
+        p_rotation = None
         if rotation is not None:
             if rotation.dim() != 2:
                 _refuse("rotation must be [max_position, rot_dim]")
-            self._dense(rotation, torch.float32, rotation.shape, "rotation")
-            a.max_position, a.rot_dim = rotation.shape
+            p_rotation = self._dense(rotation, torch.float32, rotation.shape, "rotation")
+            most, rot_dim = rotation.shape
             if positions is None:
                 _refuse("rotation without positions")
-        self._i32(positions, (B, n), "positions")
-        for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-            if w is not None:
-                self._dense(w, self.dtype, (self.D,), name)
-        self._pages(k_cache, "k_cache"), self._pages(v_cache, "v_cache")
-        ts = dict(q=q, k=k, v=v, q_out=out, slots=slots, positions=positions, rotation=rotation,
-                  q_weight=q_weight, k_weight=k_weight, k_cache=k_cache, v_cache=v_cache)
-        for name, t in ts.items():
-            setattr(a, name, None if t is None else t.data_ptr())
-        self._launch(stream, ts.values(),
-                     lambda s: _LIB.rheo_cache_write(self._h, ctypes.byref(a), s))
+        a = WriteArgs(
+            n, rot_dim, most, int(interleaved), p_q or None, p_k, p_v, p_out or None, q_row, k_row,
+            v_row, out_row, self._dense(slots, torch.int64, (B, n), "slots"),
+            self._i32(positions, (B, n), "positions"), p_rotation,
+            None if q_weight is None else self._dense(q_weight, self.dtype, dim, "q_weight"),
+            None if k_weight is None else self._dense(k_weight, self.dtype, dim, "k_weight"),
+            float(eps), self._pages(k_cache, "k_cache"), self._pages(v_cache, "v_cache"))
+        _check(_LIB.rheo_cache_write(
+            self._h, ctypes.byref(a),
+            self._stream(stream, (q, k, v, out, slots, positions, rotation, q_weight, k_weight,
+                                  k_cache, v_cache))))
         return out
 
     def attention(self, q, k_cache, v_cache, table, lens, mask=None, tail=None, count=None,
@@ -442,48 +462,48 @@ class Cache(_OnDevice):
         tail] uint8 names; without a mask, causal.  Returns out, or (out, lse) where lse is
         True or a tensor [B, n, heads] float32.  scale: 1 / sqrt(head_dim) by default."""
         B, n = self.B, q.shape[1]
-        a = AttentionArgs(n=n, scale=float(self.D ** -0.5 if scale is None else scale))
-        a.q_stride = self._rows(q, n, self.H, "q")
-        if mask is not None:
-            a.tail = mask.shape[-1] if tail is None else tail
-            self._dense(mask, torch.uint8, (B, n, a.tail), "mask")
-        else:
-            a.tail = n if tail is None else tail
-        self._pages(k_cache, "k_cache"), self._pages(v_cache, "v_cache")
-        self._i32(table, (B, self.width), "table")
-        self._i32(lens, (B,), "lens"), self._i32(count, (B,), "count")
+        p_q, q_row = self._rows(q, n, self.H, "q")
+        if tail is None:
+            tail = n if mask is None else mask.shape[-1]
+        p_table = self._i32(table, (B, self.width), "table")
+        p_mask = None
+        if mask is not None:         # (one without columns has no address, but names nothing)
+            p_mask = self._dense(mask, torch.uint8, (B, n, tail), "mask") or p_table
         if out is None:
             out = torch.empty((B, n, self.H, self.D), dtype=self.dtype, device=self.device)
-        a.out_stride = self._rows(out, n, self.H, "out")
-        both = lse is not None and lse is not False
-        lse = self._out(None if lse is True else lse, torch.float32, (B, n, self.H), "lse") \
-            if both else None
-        # (an empty mask stands for one that names nothing)
-        ts = dict(q=q, k_cache=k_cache, v_cache=v_cache, table=table, lens=lens, count=count,
-                  out=out, lse=lse)
-        for name, t in ts.items():
-            setattr(a, name, None if t is None else t.data_ptr())
-        if mask is not None:
-            a.mask = mask.data_ptr() or table.data_ptr()
-        self._launch(stream, list(ts.values()) + [mask],
-                     lambda s: _LIB.rheo_tree_attention(self._h, ctypes.byref(a), s))
+        p_out, out_row = self._rows(out, n, self.H, "out")
+        both, p_lse = lse is not None and lse is not False, None
+        if both:
+            lse, p_lse = self._made(None if lse is True else lse, torch.float32, (B, n, self.H),
+                                    "lse")
+        a = AttentionArgs(
+            n, tail, p_q, q_row, out_row, self._pages(k_cache, "k_cache"),
+            self._pages(v_cache, "v_cache"), p_table, self._i32(lens, (B,), "lens"),
+            self._i32(count, (B,), "count"), p_mask,
+            float(self.D ** -0.5 if scale is None else scale), p_out, p_lse)
+        _check(_LIB.rheo_tree_attention(
+            self._h, ctypes.byref(a),
+            self._stream(stream, (q, k_cache, v_cache, table, lens, count, mask, out,
+                                  lse if both else None))))
         return (out, lse) if both else out
 
     def commit(self, parent, token, accepted, accept_len, lens, table, k_cache, v_cache,
                out=None, stream=None):
         """Moves the entries of the accepted path together in all layers; (path [B, depth +
         1] int32, new lens [B] int32).  ``out``'s second tensor may be lens itself."""
-        B, n, depth = self.B, parent.shape[-1], accepted.shape[-1]
-        self._i32(parent, (B, n), "parent"), self._i32(token, (B, n), "token")
-        self._i32(accepted, (B, depth), "accepted"), self._i32(accept_len, (B,), "accept_len")
-        self._i32(lens, (B,), "lens"), self._i32(table, (B, self.width), "table")
-        self._pages(k_cache, "k_cache", self.layers), self._pages(v_cache, "v_cache", self.layers)
+        B, n, depth, i32 = self.B, parent.shape[-1], accepted.shape[-1], self._i32
+        one, rows = (B,), (B, n)
         path, new_lens = out or (None, None)
-        path = self._out(path, torch.int32, (B, depth + 1), "path")
-        new_lens = self._out(new_lens, torch.int32, (B,), "new_lens")
-        ts = (parent, token, accepted, accept_len, lens, table, k_cache, v_cache, path, new_lens)
-        self._launch(stream, ts, lambda s: _LIB.rheo_cache_commit(
-            self._h, n, depth, *[_ptr(t) for t in ts], s))
+        path, p_path = self._made(path, torch.int32, (B, depth + 1), "path")
+        new_lens, p_new = self._made(new_lens, torch.int32, one, "new_lens")
+        _check(_LIB.rheo_cache_commit(
+            self._h, n, depth, i32(parent, rows, "parent"), i32(token, rows, "token"),
+            i32(accepted, (B, depth), "accepted"), i32(accept_len, one, "accept_len"),
+            i32(lens, one, "lens"), i32(table, (B, self.width), "table"),
+            self._pages(k_cache, "k_cache", self.layers),
+            self._pages(v_cache, "v_cache", self.layers), p_path, p_new,
+            self._stream(stream, (parent, token, accepted, accept_len, lens, table, k_cache,
+                                  v_cache, path, new_lens))))
         return path, new_lens
 
     def device_error(self):
@@ -498,7 +518,7 @@ class Scorer(_OnDevice):
     def __init__(self, vocab, dtype, row_stride=None, device="cuda"):
         lib = load_library()
         code = _dtype_code(dtype)
-        self.device = self._device_of(device)
+        self._set_device(device)
         self._destroy = lib.rheo_scorer_destroy
         self.V, self.dtype, self.row_stride = vocab, dtype, row_stride or vocab
         self._open(lambda h: lib.rheo_scorer_create(vocab, code, self.row_stride, h))
@@ -510,21 +530,20 @@ class Scorer(_OnDevice):
         are left as they were (new outputs: zeros)."""
         if not isinstance(logits, torch.Tensor) or logits.dim() != 3:
             _refuse("logits must be a tensor [B, n, row_stride]")
-        B, n = logits.shape[:2]
-        m = tokens.shape[-1]
-        self._dense(logits, self.dtype, (B, n, self.row_stride), "logits")
-        self._dense(tokens, torch.int32, (B, m), "tokens")
-        if path is not None:
-            self._dense(path, torch.int32, (B, m), "path")
         if not 0 <= top <= 32:
             _refuse("top must be in [0, 32]")
-        want = [("logprob", torch.float32, (B, m)), ("entropy", torch.float32, (B, m)),
-                ("rank", torch.int32, (B, m)), ("top_token", torch.int32, (B, m, top)),
-                ("top_logprob", torch.float32, (B, m, top))]
+        B, n = logits.shape[:2]
+        m = tokens.shape[-1]
+        one, best = (B, m), (B, m, top)
+        want = (("logprob", torch.float32, one), ("entropy", torch.float32, one),
+                ("rank", torch.int32, one), ("top_token", torch.int32, best),
+                ("top_logprob", torch.float32, best))
         if out is None:
-            out = [torch.zeros(s, dtype=d, device=self.device) for _, d, s in want]
-        out = tuple(self._dense(t, d, s, name) for t, (name, d, s) in zip(out, want))
-        self._launch(stream, (logits, path, tokens) + out, lambda s: _LIB.rheo_token_logprobs(
-            self._h, _ptr(logits), B, n, _ptr(path), _ptr(tokens), m, top, float(T),
-            *[_ptr(t) for t in out], s))
-        return out
+            out = tuple(torch.zeros(s, dtype=d, device=self.device) for _, d, s in want)
+        _check(_LIB.rheo_token_logprobs(
+            self._h, self._dense(logits, self.dtype, (B, n, self.row_stride), "logits"), B, n,
+            None if path is None else self._dense(path, torch.int32, one, "path"),
+            self._dense(tokens, torch.int32, one, "tokens"), m, top, float(T),
+            *[self._dense(t, d, s, name) for t, (name, d, s) in zip(out, want)],
+            self._stream(stream, (logits, path, tokens, *out))))
+        return tuple(out)

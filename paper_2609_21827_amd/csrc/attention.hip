@@ -783,9 +783,6 @@ hipError_t start(AttnArgs p, hipStream_t s) {
     static_assert(S::LDS <= 156 * 1024, "LDS");
     p.groups = p.c.slots * S::RESIDENT;
     p.min_tiles = 1;
-    const void* fn = (const void*)k_tree_attention<T, S>;
-    hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
-    if (e != hipSuccess) return e;
     k_tree_attention<T, S><<<p.groups, S::NT, S::LDS, s>>>(p);
     // Items that are cut once or twice take a wave a block of 32 elements, those of
     // which many stretches have a part eight waves
@@ -815,7 +812,31 @@ hipError_t start_dim(const AttnArgs& p, hipStream_t s) {
     return start_rows<T, 256>(p, s);
 }
 
+template <typename T, typename S>
+hipError_t allow_lds() {
+    return hipFuncSetAttribute((const void*)k_tree_attention<T, S>,
+                               hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+}
+
+template <typename T, int DT>
+hipError_t prepare_dim() {
+    typedef Shapes<DT> H;
+    hipError_t e = allow_lds<T, typename H::R1>();
+    if (e == hipSuccess) e = allow_lds<T, typename H::R2>();
+    if (e == hipSuccess) e = allow_lds<T, typename H::R4>();
+    return e == hipSuccess ? allow_lds<T, typename H::R8>() : e;
+}
+
+template <typename T>
+hipError_t prepare_type(int D) {
+    return D <= 64 ? prepare_dim<T, 64>() : D <= 128 ? prepare_dim<T, 128>() : prepare_dim<T, 256>();
+}
+
 }  // namespace
+
+hipError_t prepare_attention(const CacheDev& c) {
+    return c.dtype == RHEO_BF16 ? prepare_type<__bf16>(c.D) : prepare_type<_Float16>(c.D);
+}
 
 size_t attention_workspace(const CacheDev& c) {
     const size_t n = c.D <= 64 ? workspace<64>(c.slots) : c.D <= 128 ? workspace<128>(c.slots)

@@ -114,6 +114,8 @@ int rheo_cache_create(const rheo_cache_config* cfg, rheo_cache** out) {
     if (rc == RHEO_OK) rc = zeroed((void**)&d.err, sizeof(int32_t));
     if (rc == RHEO_OK) rc = zeroed((void**)&d.ticket, (d.B + 1) * sizeof(uint32_t));
     if (rc == RHEO_OK) rc = zeroed((void**)&d.part, attention_workspace(d) * sizeof(float));
+    if (rc == RHEO_OK && (e = prepare_attention(d)) != hipSuccess)
+        rc = hip_fail(e, "tree attention set-up");
     if (rc == RHEO_OK && (e = hipDeviceSynchronize()) != hipSuccess)
         rc = hip_fail(e, "initialising a workspace");
     if (rc != RHEO_OK) {

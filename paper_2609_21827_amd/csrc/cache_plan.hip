@@ -13,9 +13,8 @@ struct Demand {
     bool valid;
 };
 
-__device__ __forceinline__ Demand demand_of(const CacheDev& c, const PlanArgs& a, int b) {
-    const int len = a.lens[b], held = a.held[b];
-    const int count = a.count ? a.count[b] : a.n;
+__device__ __forceinline__ Demand demand_of(const CacheDev& c, const PlanArgs& a, int len, int count,
+                                            int held) {
     Demand d;
     d.valid = len >= 0 && count >= 0 && count <= a.n && held >= 0 && held <= c.width;
     const int64_t need = ((int64_t)len + count + (1 << c.page_shift) - 1) >> c.page_shift;
@@ -57,15 +56,26 @@ __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
     const int have0 = *a.free_count;
     int64_t take = 0, give = 0;
     bool bad = false;
-#pragma unroll 4
-    for (int b = b0; b < b1; ++b) {
-        const Demand d = demand_of(c, a, b);
-        s_take[b] = clamp31(take);           // (relative to the thread's first)
-        s_give[b] = clamp31(give);
-        s_need[b] = d.fits ? d.need : -1;
-        take += d.take;
-        give += d.give;
-        bad |= !d.valid;
+    for (int b = b0; b < b1; b += 4) {
+        int len[4], count[4], held[4];       // (the last sequence's again past the end)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = min(b + k, b1 - 1);
+            len[k] = a.lens[i];
+            count[k] = a.count ? a.count[i] : a.n;
+            held[k] = a.held[i];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (b + k >= b1) break;
+            const Demand d = demand_of(c, a, len[k], count[k], held[k]);
+            s_take[b + k] = clamp31(take);   // (relative to the thread's first)
+            s_give[b + k] = clamp31(give);
+            s_need[b + k] = d.fits ? d.need : -1;
+            take += d.take;
+            give += d.give;
+            bad |= !d.valid;
+        }
     }
     int64_t ti = take, gi = give;
     for (int o = 1; o < 64; o <<= 1) {
@@ -131,9 +141,9 @@ __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
         for (int p = tid % 16; p < took; p += 16)
             a.table[(int64_t)b * c.width + held + p] = stack_page(room - 1 - s_take[b] - p);
     }
-    const int64_t rows = (int64_t)mine * a.n;
-    for (int64_t f = tid; f < rows; f += NTP) {
-        const int k = (int)(f / a.n), i = (int)(f - (int64_t)k * a.n);
+    const int rows = mine * a.n;               // (at most 2^30)
+    for (int f = tid; f < rows; f += NTP) {
+        const int k = f / a.n, i = f - k * a.n;
         const int b = blockIdx.x + k * gridDim.x;
         const int64_t at = (int64_t)b * a.n + i;
         const int len = a.lens[b], count = a.count ? a.count[b] : a.n;

@@ -42,6 +42,8 @@ hipError_t launch_cache_plan(const CacheDev& c, const PlanArgs& a, hipStream_t s
 hipError_t launch_cache_write(const CacheDev& c, const rheo_write_args& a, hipStream_t s);
 hipError_t launch_tree_attention(const CacheDev& c, const rheo_attention_args& a, hipStream_t s);
 hipError_t launch_cache_commit(const CacheDev& c, const CommitArgs& a, hipStream_t s);
+// once for the current device, before the first launch
+hipError_t prepare_attention(const CacheDev& c);
 // floats of partial results that launch_tree_attention may write
 size_t attention_workspace(const CacheDev& c);
 
