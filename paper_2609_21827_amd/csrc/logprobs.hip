@@ -22,7 +22,8 @@ constexpr float kLn2 = 0.69314718055994531f;
 
 // What a row, or a part of it, comes to: the largest logit, and with t = (l -
 // max) log2(e) / T the sums of 2^t and t 2^t; the number of tokens before the
-// given one.
+// given one.  (t as one fused l kT - max kT would save an instruction of twelve,
+// but the maximum's own t would not be 0, nor a sure token's log probability.)
 struct Stat {
     float m, s, st;
     int before;
@@ -70,9 +71,8 @@ __device__ __forceinline__ void unpack_vec(const uint4& v, float* x) {
     }
 }
 
-// Sums relative to a larger maximum: with d = (m - ref) kT <= 0, 2^t becomes
-// 2^t 2^d and t 2^t becomes (t + d) 2^t 2^d.  Nothing counted yet (m = -inf):
-// both sums are 0.
+// Sums relative to a larger maximum: with d = (m - m') kT <= 0, 2^t becomes 2^t 2^d
+// and t 2^t becomes (t + d) 2^t 2^d.  Nothing counted yet (m = -inf): both are 0.
 __device__ __forceinline__ void rebase(Stat& a, float m, float kT) {
     if (!(a.m < m)) return;
     const float d = a.m == -INFINITY ? 0.0f : (a.m - m) * kT;
@@ -154,14 +154,12 @@ __device__ __forceinline__ void put_outputs(const LogprobArgs& a, int entry, con
 // rise) is looked at again with its top-th largest key, found bit by bit over
 // the registers: at most `top` are that large.
 //
-// Bound by the row's bytes: 128 x 5 rows of 151936 bf16, 4 to 5 of 9 there
-// (MEASURED_HERE).
 template <int DT>
 __global__ __launch_bounds__(NTL) void k_row_stats(ScoreDev c, LogprobArgs a, int segs,
                                                    int seg_chunks) {
     __shared__ uint64_t s_list[LIST], s_best[TOP];
     __shared__ Stat s_stat[NWL];
-    __shared__ int s_sum[NWL], s_cnt;
+    __shared__ int s_sum[NWL], s_cnt[3];
     __shared__ uint32_t s_bound[NWL];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int entry = blockIdx.x / segs, seg = blockIdx.x - entry * segs;
@@ -179,10 +177,11 @@ __global__ __launch_bounds__(NTL) void k_row_stats(ScoreDev c, LogprobArgs a, in
 #pragma unroll
     for (int v = 0; v < NV; ++v) next[v] = load_vec<DT>(row, first + (v * NTL + tid) * VEC, V);
     const float lt = (float)((const Elem<DT>*)row)[token];
-    if (tid == 0) s_cnt = 0;
+    if (tid < 3) s_cnt[tid] = 0;
     __syncthreads();
 
     Stat st = {-INFINITY, 0.0f, 0.0f, 0};
+    int before = 0;                        // of the wave
     int listed = 0;                        // keys in s_list
     uint64_t over = 0;                     // keys above it go in,
     float low = 0.0f;                      // of logits at least that large
@@ -198,13 +197,15 @@ __global__ __launch_bounds__(NTL) void k_row_stats(ScoreDev c, LogprobArgs a, in
         listed = min(listed, top);
         __syncthreads();
         if (tid < listed) s_list[tid] = s_best[tid];
-        if (tid == 0) s_cnt = listed;
         if (listed == top) {
             over = s_best[top - 1];
             low = key_value(over);
         }
         __syncthreads();
     };
+    // keys that a chunk adds are counted in one of three places, so that one barrier a
+    // chunk is enough: a place is cleared between the barriers after its last use
+    int turn = 0;
     for (int c0 = first; c0 < end; c0 += CHUNK) {
         float x[EPT];
 #pragma unroll
@@ -228,17 +229,19 @@ __global__ __launch_bounds__(NTL) void k_row_stats(ScoreDev c, LogprobArgs a, in
             st.s += e;
             st.st = __fmaf_rn(t, e, st.st);
         }
-        // a tie goes before the token where its id is lower
+        // tokens before the given one, a wave's by ballot: a tie goes before it where
+        // its id is lower
         if (c0 + CHUNK <= token) {
 #pragma unroll
-            for (int k = 0; k < EPT; ++k) st.before += x[k] >= lt;
+            for (int k = 0; k < EPT; ++k) before += __builtin_popcountll(__ballot(x[k] >= lt));
         } else if (c0 > token) {
 #pragma unroll
-            for (int k = 0; k < EPT; ++k) st.before += (x[k] > lt) & (id_of(k) < V);
+            for (int k = 0; k < EPT; ++k) before += __builtin_popcountll(__ballot(x[k] > lt));
         } else {
 #pragma unroll
             for (int k = 0; k < EPT; ++k)
-                st.before += (x[k] > lt) | ((x[k] == lt) & (id_of(k) < token));
+                before += __builtin_popcountll(
+                    __ballot((x[k] > lt) | ((x[k] == lt) & (id_of(k) < token))));
         }
         if (top == 0) continue;
 
@@ -257,7 +260,7 @@ __global__ __launch_bounds__(NTL) void k_row_stats(ScoreDev c, LogprobArgs a, in
         auto list = [&](int k) {
             const uint64_t key = logit_key(x[k], (uint32_t)id_of(k));
             if (key > over && id_of(k) < V) {
-                const int at = atomicAdd(&s_cnt, 1);
+                const int at = listed + atomicAdd(&s_cnt[turn], 1);
                 if (at < LIST) s_list[at] = key;
             }
         };
@@ -266,16 +269,16 @@ __global__ __launch_bounds__(NTL) void k_row_stats(ScoreDev c, LogprobArgs a, in
 #pragma unroll
             for (int k = 0; k < EPT; ++k)
                 if (x[k] >= low) list(k);
+        if (tid == 0) s_cnt[turn == 2 ? 0 : turn + 1] = 0;
         __syncthreads();
-        const int total = s_cnt;
+        const int total = listed + s_cnt[turn];
+        turn = turn == 2 ? 0 : turn + 1;
         if (total <= LIST) {
             listed = total;
             if (c0 == first || total > 2 * top + 16) rank();
-            else __syncthreads();          // (s_cnt has been read)
             continue;
         }
         // this chunk's keys are not all in: without them, then its best alone
-        __syncthreads();
         rank();
         const int k_th = min(top, min(V - c0, CHUNK));
         uint64_t t = 0;
@@ -293,14 +296,16 @@ __global__ __launch_bounds__(NTL) void k_row_stats(ScoreDev c, LogprobArgs a, in
         for (int k = 0; k < EPT; ++k)
             if (x[k] >= low) list(k);
         __syncthreads();
-        listed = s_cnt;
+        listed += s_cnt[turn];
         __syncthreads();
-        rank();
+        if (tid == 0) s_cnt[turn] = 0;
+        rank();                            // (with a barrier before the place's next use)
     }
     if (top) rank();
     const int best = listed;
 
     st = wave_join(st, kT);
+    st.before = before;
     if (lane == 0) s_stat[wave] = st;
     __syncthreads();
     if (wave) return;
