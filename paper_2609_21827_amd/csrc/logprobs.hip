@@ -11,13 +11,13 @@ namespace rheo {
 
 namespace {
 
-constexpr int NTL = 512;                  // threads of a block
+constexpr int NTL = 256;                  // threads of a block
 constexpr int NWL = NTL / 64;
 constexpr int EPT = 16;                   // elements a thread holds of a chunk
-constexpr int CHUNK = NTL * EPT;          // 8192 elements
+constexpr int CHUNK = NTL * EPT;          // 4096 elements
 constexpr int TOP = 32;                   // most alternatives
 constexpr int LIST = 1024;                // most candidates of a chunk
-constexpr int PARTS = 1024;               // most segments of a launch that splits rows
+constexpr int PARTS = 2400;               // most segments of a launch that splits rows
 constexpr float kLn2 = 0.69314718055994531f;
 
 // What a row, or a part of it, comes to: the largest logit, and with t = (l -
@@ -336,12 +336,14 @@ __global__ __launch_bounds__(64) void k_row_join(ScoreDev c, LogprobArgs a, int 
     const Stat st = wave_join(has ? p->stat : Stat{-INFINITY, 0.0f, 0.0f, 0}, a.kT);
     uint64_t head = has && a.top ? p->key[0] : 0, best = 0;
     int at = 0;
+    const int wide = segs > 1 ? 1 << (31 - __builtin_clz(segs - 1)) : 0;    // lanes that compare
     for (int i = 0; i < a.top; ++i) {
         uint64_t m = head;
-        for (int o = 32; o; o >>= 1) {
+        for (int o = wide; o; o >>= 1) {
             const uint64_t u = __shfl_xor(m, o);
             m = u > m ? u : m;
         }
+        m = lane_u64(m, 0);
         if (lane == i) best = m;
         if (head == m && m) head = ++at < a.top ? p->key[at] : 0;
     }
@@ -353,8 +355,12 @@ namespace {
 template <int DT>
 hipError_t start(const ScoreDev& c, const LogprobArgs& a, hipStream_t s) {
     const int entries = a.B * a.m, chunks = (c.V + CHUNK - 1) / CHUNK;
-    // Rows are split while their segments are few enough to need each other's
-    // compute units, into at most 64 (a lane each in the join)
+    // Rows are split while all segments stay below PARTS, eight or nine blocks a
+    // compute unit, into at most 64 (a lane each in the join).  Splitting costs a
+    // first chunk's selection a segment and the join: 640 rows of 151936, 20
+    // alternatives, 79 us in one to three parts each and 85 in six; but 1152 entries of
+    // which half are left out 95 us whole and 80 in halves, since whole they leave
+    // most of the chip's waves unused.
     int segs = PARTS / entries;
     segs = segs < 1 ? 1 : segs > 64 ? 64 : segs;
     if (segs > chunks) segs = chunks;
