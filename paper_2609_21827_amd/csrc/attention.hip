@@ -269,7 +269,7 @@ template <typename S>
 struct Rows {
     u32x4 q[S::KS];                // Q^T: the lane's row, elements 16s + 8h + (0..7)
     f32x16 o[S::DB];               // O^T: row, elements 32db + 8(r/4) + 4h + r%4
-    float m, l;                    // its maximum score so far; its half's sum
+    float m, l;                    // the exponents' reference, a score; its half's sum
 };
 
 }  // namespace
@@ -287,6 +287,7 @@ k_tree_attention(AttnArgs p) {
     const rheo_attention_args& a = p.a;
     const int w = blockIdx.x, D = c.D;
     const float to2 = a.scale * kLog2e;              // scores to exponents of 2
+    const float slack = 8.0f / to2;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_lds;
     const uint32_t lds_mine = __builtin_amdgcn_readfirstlane(lds0 + wave * (S::J * 1024));
     const uint32_t lds_pages = __builtin_amdgcn_readfirstlane(lds0 + S::RING + wave * 256);
@@ -437,8 +438,6 @@ k_tree_attention(AttnArgs p) {
             }
             // (with one row block a wave works on the rows it has loaded itself)
             if (S::RT > 1) __syncthreads();
-            if (t + S::P < end_tile) fetch(t + S::P);
-            if (t + 2 * S::P < end_tile) fetch_pages(t + 2 * S::P);
 
             // S^T of the wave's U blocks of 32 entries
             const int e0 = kw * S::U * 32;           // (of the tile)
@@ -460,6 +459,9 @@ k_tree_attention(AttnArgs p) {
                 __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
             __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
+            // (the products are under way: time for the loads' addresses)
+            if (t + S::P < end_tile) fetch(t + S::P);
+            if (t + 2 * S::P < end_tile) fetch_pages(t + 2 * S::P);
             if (tail_tile) {
                 const int eh = t * S::KT + e0 + 4 * half;
                 if (mrow && sq.tail > 0) {
@@ -486,7 +488,10 @@ k_tree_attention(AttnArgs p) {
                             sc[u][i] = eh + u * 32 + 8 * (i / 4) + i % 4 < end ? sc[u][i] : -INFINITY;
                 }
             }
-            // running maximum and sum
+            // The exponents' reference is the row's maximum so far, or lower by up to 8:
+            // probabilities are then at most 2^8, which all that holds them takes, and
+            // O is rescaled once or twice an item instead of at most tiles (some row of
+            // 32 has a new maximum).
             float mx = sc[0][0];
 #pragma unroll
             for (int u = 0; u < S::U; ++u)
@@ -494,14 +499,15 @@ k_tree_attention(AttnArgs p) {
                 for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[u][i]);
             const f32x2 mb = both_halves(mx);
             const float m = fmaxf(x.m, fmaxf(mb[0], mb[1]));
-            const float ref = m == -INFINITY ? 0.0f : m * to2;
-            if (__any(m > x.m)) {
-                const float f = __builtin_amdgcn_exp2f(__fmaf_rn(x.m, to2, -ref));
+            if (__any(m > x.m + slack)) {
+                const float f = __builtin_amdgcn_exp2f(
+                    __fmaf_rn(x.m, to2, m == -INFINITY ? 0.0f : -m * to2));
                 x.l *= f;
 #pragma unroll
                 for (int d = 0; d < S::DB; ++d) x.o[d] *= f;
+                x.m = m;
             }
-            x.m = m;
+            const float ref = x.m == -INFINITY ? 0.0f : x.m * to2;
             float sum = 0.0f;
 #pragma unroll
             for (int u = 0; u < S::U; ++u)
@@ -737,29 +743,34 @@ __global__ __launch_bounds__(NTJ) void k_attn_join(AttnArgs p) {
 
 namespace {
 
-// Shapes for up to 32, 64, 128 and more rows of an item.
+// Shapes for up to 32, 64, 128 and more rows of an item: the fastest of those that
+// fit, of two or three tried each.  Few rows are bound by memory, and the waves of
+// a workgroup share the entries; many by the products and the vector work between
+// them.  us for 32 sequences, 8 key heads of 128, 4096 entries (bytes: 64 at the
+// copy's rate) with 4 rows 82 (two waves, three tiles ahead: 86), 40 rows 90 (eight
+// waves: 126; one tile ahead: 115), 100 rows 118 (eight waves: 135), 244 rows 157.
 template <int DT>
 struct Shapes;
 template <>
 struct Shapes<64> {
-    typedef Shape<64, 1, 4, 1, 3> R1;
+    typedef Shape<64, 1, 4, 1, 1> R1;
     typedef Shape<64, 2, 4, 1, 3> R2;
-    typedef Shape<64, 4, 8, 1, 3> R4;
+    typedef Shape<64, 4, 4, 2, 3> R4;
     typedef Shape<64, 8, 8, 2, 3> R8;
 };
 template <>
 struct Shapes<128> {
-    typedef Shape<128, 1, 2, 1, 3> R1;
+    typedef Shape<128, 1, 4, 1, 1> R1;
     typedef Shape<128, 2, 4, 1, 3> R2;
-    typedef Shape<128, 4, 8, 1, 3> R4;
+    typedef Shape<128, 4, 4, 2, 3> R4;
     typedef Shape<128, 8, 8, 2, 3> R8;
 };
 template <>
 struct Shapes<256> {
-    typedef Shape<256, 1, 2, 1, 1> R1;
     typedef Shape<256, 2, 2, 1, 3> R2;
+    typedef R2 R1;                 // (two waves on 32 rows, one tile ahead: 168 us for 120)
     typedef Shape<256, 4, 4, 1, 3> R4;
-    typedef R4 R8;
+    typedef R4 R8;                 // (256 rows of 256 do not fit the registers)
 };
 
 template <typename S>

@@ -131,10 +131,10 @@ def logprobs(row, token, top, T):
     order = torch.sort(x, descending=True, stable=True)[1]
     rank = int((order == token).nonzero()[0, 0])
     ids = order[:top]
-    # fp32: a thread adds at most 16 terms a chunk of 8192, a block's and the
+    # fp32: a thread of 256 adds at most V / 256 terms and 16, a block's and the
     # segments' results are joined in 16 more steps; an exponent is off by a few
     # roundings of itself, which weigh as much as the terms do
-    adds = 16 * -(-V // 8192) + 32
+    adds = V // 256 + 32
     spread = float((p * torch.where(p > 0, (x - x.max()).abs() / T, torch.zeros_like(p))).sum())
     base = U32 * (adds + 8 * spread + 16)
     bound = lambda y: base + 8 * U32 * (y.abs() + float(-logp.max()))  # noqa: E731
