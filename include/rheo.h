@@ -297,6 +297,7 @@ int32_t rheo_node_count(const rheo_tree* tree);
  * Lengths, tables, slots and tokens are data that the host cannot check: a
  * value out of range sets a bit of the error flag (rheo_cache_error) and
  * never reads or writes outside the arrays as declared by the arguments.
+ * n = 0 rows: rheo_cache_write and rheo_tree_attention do nothing.
  * ------------------------------------------------------------------------ */
 
 typedef struct rheo_cache rheo_cache;

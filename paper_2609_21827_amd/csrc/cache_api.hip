@@ -178,6 +178,7 @@ int rheo_cache_write(rheo_cache* c, const rheo_write_args* args, void* stream) {
     if (a.interleaved != 0 && a.interleaved != 1)
         return fail(RHEO_EINVAL, "interleaved must be 0 or 1");
     if (!(a.eps >= 0.0f) || !std::isfinite(a.eps)) return fail(RHEO_EINVAL, "eps must be >= 0");
+    if (a.n == 0) return RHEO_OK;            // (empty arrays may have no address)
     if (!a.q != !a.q_out) return fail(RHEO_EINVAL, "q and q_out: both or none");
     if (a.q) {
         if ((rc = check_ptr(a.q, "q")) || (rc = check_ptr(a.q_out, "q_out"))) return rc;
@@ -198,7 +199,6 @@ int rheo_cache_write(rheo_cache* c, const rheo_write_args* args, void* stream) {
     if (a.q_weight && (rc = check_ptr(a.q_weight, "q_weight"))) return rc;
     if (a.k_weight && (rc = check_ptr(a.k_weight, "k_weight"))) return rc;
     if ((rc = check_ptr(a.k_cache, "k_cache")) || (rc = check_ptr(a.v_cache, "v_cache"))) return rc;
-    if (a.n == 0) return RHEO_OK;
     OnDevice on(c->device);
     if (on.error() != hipSuccess) return hip_fail(on.error(), "hipSetDevice");
     return launched(launch_cache_write(d, a, (hipStream_t)stream), "cache write launch");
@@ -216,6 +216,7 @@ int rheo_tree_attention(rheo_cache* c, const rheo_attention_args* args, void* st
     if (!a.mask && a.tail < a.n) return fail(RHEO_EINVAL, "tail must be >= n without a mask");
     if (!(a.scale > 0.0f) || !std::isfinite(a.scale))
         return fail(RHEO_EINVAL, "scale must be finite and > 0");
+    if (a.n == 0) return RHEO_OK;            // (empty arrays may have no address)
     if ((rc = check_ptr(a.q, "q")) || (rc = check_ptr(a.out, "out"))) return rc;
     if ((rc = check_stride(a.q_stride, (int64_t)d.H * d.D, "q_stride"))) return rc;
     if ((rc = check_stride(a.out_stride, (int64_t)d.H * d.D, "out_stride"))) return rc;
@@ -224,7 +225,6 @@ int rheo_tree_attention(rheo_cache* c, const rheo_attention_args* args, void* st
     if ((rc = check_words(a.table, 4, "table")) || (rc = check_words(a.lens, 4, "lens"))) return rc;
     if (a.count && (rc = check_words(a.count, 4, "count"))) return rc;
     if (a.lse && (rc = check_words(a.lse, 4, "lse"))) return rc;
-    if (a.n == 0) return RHEO_OK;
     OnDevice on(c->device);
     if (on.error() != hipSuccess) return hip_fail(on.error(), "hipSetDevice");
     return launched(launch_tree_attention(d, a, (hipStream_t)stream), "tree attention launch");

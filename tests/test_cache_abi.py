@@ -1,0 +1,74 @@
+"""The cache and scoring calls without a GPU: configurations and arguments that are
+refused on the host before any device call."""
+
+import ctypes
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_2609_21827_amd", "librheo.so")
+needs_lib = pytest.mark.skipif(not os.path.exists(LIB), reason="librheo.so not built")
+
+GOOD = dict(batch=2, heads=8, kv_heads=2, head_dim=128, page_size=16, pages=10, table_width=4,
+            layers=2, dtype=1, page_stride=0, layer_stride=0)
+BAD = [
+    dict(batch=0), dict(batch=4097), dict(kv_heads=0), dict(heads=0), dict(heads=7),
+    dict(heads=1032, kv_heads=8), dict(head_dim=0), dict(head_dim=12), dict(head_dim=264),
+    dict(page_size=0), dict(page_size=24), dict(page_size=8192), dict(pages=0),
+    dict(table_width=0), dict(table_width=1 << 27), dict(layers=0), dict(layers=1025),
+    dict(dtype=0), dict(dtype=3), dict(page_stride=16 * 2 * 128 - 8), dict(page_stride=16 * 2 * 128 + 4),
+    dict(page_stride=1 << 41), dict(layer_stride=1), dict(layer_stride=10 * 16 * 2 * 128 + 4),
+    dict(layer_stride=9 * 16 * 2 * 128),
+]
+
+
+@needs_lib
+@pytest.mark.parametrize("bad", BAD)
+def test_invalid_cache_configs_are_refused(bad):
+    from paper_2609_21827_amd import binding
+    lib = binding.load_library()
+    h = ctypes.c_void_p()
+    cfg = binding.CacheConfig(**{**GOOD, **bad})
+    assert lib.rheo_cache_create(ctypes.byref(cfg), ctypes.byref(h)) == binding.RHEO_EINVAL
+    assert not h.value and lib.rheo_last_error().decode()
+
+
+@needs_lib
+@pytest.mark.parametrize("vocab,dtype,stride", [(1, 1, 8), (0, 1, 8), ((1 << 24) + 1, 1, 1 << 25),
+                                                (1000, 3, 1000), (1000, -1, 1000), (1000, 1, 992),
+                                                (1000, 1, 1001), (1000, 0, 1002),
+                                                (1000, 1, 1 << 33)])
+def test_invalid_scorers_are_refused(vocab, dtype, stride):
+    from paper_2609_21827_amd import binding
+    lib = binding.load_library()
+    h = ctypes.c_void_p()
+    assert lib.rheo_scorer_create(vocab, dtype, stride, ctypes.byref(h)) == binding.RHEO_EINVAL
+    assert not h.value and lib.rheo_last_error().decode()
+
+
+@needs_lib
+def test_null_handles_are_refused():
+    from paper_2609_21827_amd import binding
+    lib = binding.load_library()
+    none, flag = [None], ctypes.c_int32(0)
+    for rc in (lib.rheo_cache_create(None, None), lib.rheo_cache_error(None, ctypes.byref(flag)),
+               lib.rheo_cache_plan(None, 1, *none * 11), lib.rheo_cache_write(None, None, None),
+               lib.rheo_tree_attention(None, None, None),
+               lib.rheo_cache_commit(None, 1, 1, *none * 11),
+               lib.rheo_scorer_create(1000, 1, 1000, None),
+               lib.rheo_token_logprobs(None, None, 1, 1, None, None, 1, 0, 1.0, *none * 6)):
+        assert rc == binding.RHEO_EINVAL and lib.rheo_last_error().decode()
+    # as rheo_destroy, nothing to do
+    assert lib.rheo_cache_destroy(None) == binding.RHEO_OK
+    assert lib.rheo_scorer_destroy(None) == binding.RHEO_OK
+
+
+@needs_lib
+def test_trees_keep_their_types():
+    """RHEO_F16 is a type of the cache and the scorer alone."""
+    from paper_2609_21827_amd import binding
+    lib = binding.load_library()
+    cfg = binding.RheoConfig(2, 1000, 4, 1, 3, 0, 128, 0, binding.RHEO_F16, 0, 0, 1000, 0.0)
+    h = ctypes.c_void_p()
+    assert lib.rheo_create(ctypes.byref(cfg), ctypes.byref(h)) == binding.RHEO_EINVAL
