@@ -310,21 +310,22 @@ typedef struct rheo_cache_config {
     int32_t page_size;           /* entries of a page: a power of two, 1..4096           */
     int32_t pages;               /* pages of the pool, >= 1                             */
     int32_t table_width;         /* pages a sequence may hold, >= 1; table_width *
-                                    page_size < 2^31                                  */
+                                    page_size <= 2^30                                 */
     int32_t layers;              /* layers one rheo_cache_commit moves, 1..1024          */
     int32_t dtype;               /* RHEO_BF16 or RHEO_F16                               */
     int64_t page_stride;         /* >= page_size * kv_heads * head_dim; 0: equal to it   */
     int64_t layer_stride;        /* >= pages * page_stride; 0: equal to it               */
 } rheo_cache_config;
 
-/* Allocates the workspace (of the current device, which becomes the handle's). */
+/* Allocates the workspace (of the current device, which becomes the handle's):
+ * some 70 MB, most of it partial results of rheo_tree_attention. */
 int rheo_cache_create(const rheo_cache_config* cfg, rheo_cache** out);
 /* Frees it (synchronises the device). */
 int rheo_cache_destroy(rheo_cache* cache);
 
 /* Synchronises the handle's device and reads its sticky error flag: bit 0:
  * lens, count, held, free_count or the free list out of range in
- * rheo_cache_plan; bit 1: a slot >= pages * page_size; bit 2: a position
+ * rheo_cache_plan, count in rheo_tree_attention; bit 1: a slot >= pages * page_size; bit 2: a position
  * outside the rotation table; bit 3: a page outside the pool; bit 4: an
  * accepted token that is no child of the node before it; bit 5: entries
  * past the table's row. */

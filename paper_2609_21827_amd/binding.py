@@ -540,6 +540,8 @@ class Scorer(_OnDevice):
                 ("top_logprob", torch.float32, best))
         if out is None:
             out = tuple(torch.zeros(s, dtype=d, device=self.device) for _, d, s in want)
+        if len(out) != len(want):
+            _refuse(f"out must be {len(want)} tensors")
         _check(_LIB.rheo_token_logprobs(
             self._h, self._dense(logits, self.dtype, (B, n, self.row_stride), "logits"), B, n,
             None if path is None else self._dense(path, torch.int32, one, "path"),

@@ -79,8 +79,9 @@ __device__ __forceinline__ Seq seq_of(const AttnArgs& p, int b) {
     Seq s;
     const int64_t room = (int64_t)p.c.width << p.c.page_shift;
     s.len = p.a.lens[b];
-    s.rows = p.a.count ? p.a.count[b] : p.a.n;
-    s.rows = min(max(s.rows, 0), p.a.n);
+    const int count = p.a.count ? p.a.count[b] : p.a.n;
+    s.rows = min(max(count, 0), p.a.n);
+    if (count != s.rows) atomicOr(p.c.err, CE_PLAN);
     s.tail = max(p.a.tail - (p.a.n - s.rows), 0);
     if (s.len < 0 || s.len + (int64_t)s.tail > room) {
         if (s.rows) atomicOr(p.c.err, CE_TABLE);
@@ -191,7 +192,7 @@ __device__ __forceinline__ f32x16 mfma(const u32x4& a, const u32x4& b, const f32
 // next to each other from `lds` on.  They are in flight until wait_loads; the
 // compiler does not know of them, which only makes its own waits longer.  (Its
 // builtin would make every LDS read wait for all of them.)  No register is
-// written.
+// written but m0, which nothing else here uses (the compiler reserves it).
 __device__ __forceinline__ void load_lds16(uint32_t lds, const void* p) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p)
                  : "memory");
@@ -500,8 +501,9 @@ k_tree_attention(AttnArgs p) {
             const f32x2 mb = both_halves(mx);
             const float m = fmaxf(x.m, fmaxf(mb[0], mb[1]));
             if (__any(m > x.m + slack)) {
+                // (both references as the exponents have them, rounded)
                 const float f = __builtin_amdgcn_exp2f(
-                    __fmaf_rn(x.m, to2, m == -INFINITY ? 0.0f : -m * to2));
+                    x.m * to2 - (m == -INFINITY ? 0.0f : m * to2));
                 x.l *= f;
 #pragma unroll
                 for (int d = 0; d < S::DB; ++d) x.o[d] *= f;
@@ -562,9 +564,9 @@ k_tree_attention(AttnArgs p) {
 #pragma unroll
             for (int k = 0; k < S::KW; ++k) {
                 const float* ml = s_ml + ((k * S::RT + rt) * 32 + col) * 2;
-                l += ml[1] * __builtin_amdgcn_exp2f(__fmaf_rn(ml[0], to2, -ref));
+                l += ml[1] * __builtin_amdgcn_exp2f(ml[0] * to2 - ref);
             }
-            const float f = __builtin_amdgcn_exp2f(__fmaf_rn(x.m, to2, -ref));
+            const float f = __builtin_amdgcn_exp2f(x.m * to2 - ref);
             float* out = (float*)s_lds;
 #pragma unroll
             for (int d = 0; d < S::DB; ++d) {
@@ -686,9 +688,9 @@ __global__ __launch_bounds__(NTJ) void k_attn_join(AttnArgs p) {
         const float m1 = k + NS < n ? q1[ml] : -INFINITY, l1 = q1[ml + 1];
         bad |= ((const int*)q0)[S::PART - 1] | ((const int*)q1)[S::PART - 1];
         const float top = fmaxf(m, fmaxf(m0, m1)), ref = top == -INFINITY ? 0.0f : top * to2;
-        const float f = __builtin_amdgcn_exp2f(__fmaf_rn(m, to2, -ref));
-        const float g0 = __builtin_amdgcn_exp2f(__fmaf_rn(m0, to2, -ref));
-        const float g1 = __builtin_amdgcn_exp2f(__fmaf_rn(m1, to2, -ref));
+        const float f = __builtin_amdgcn_exp2f(m * to2 - ref);
+        const float g0 = __builtin_amdgcn_exp2f(m0 * to2 - ref);
+        const float g1 = __builtin_amdgcn_exp2f(m1 * to2 - ref);
         m = top;
         l = l * f + l0 * g0;
         if (k + NS < n) l = __fmaf_rn(l1, g1, l);
@@ -717,7 +719,7 @@ __global__ __launch_bounds__(NTJ) void k_attn_join(AttnArgs p) {
     l = 0.0f;
     bad = 0;
     for (int k = 0; k < parts; ++k) {
-        l = __fmaf_rn(s_l[k][col], __builtin_amdgcn_exp2f(__fmaf_rn(s_m[k][col], to2, -ref)), l);
+        l = __fmaf_rn(s_l[k][col], __builtin_amdgcn_exp2f(s_m[k][col] * to2 - ref), l);
         bad |= s_flag[k];
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -729,7 +731,7 @@ __global__ __launch_bounds__(NTJ) void k_attn_join(AttnArgs p) {
         const int i = f % 4, at = 32 * (d0 + f / 4) + 8 * i + 4 * half;
         float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int k = 0; k < parts; ++k) {
-            const float g = __builtin_amdgcn_exp2f(__fmaf_rn(s_m[k][col], to2, -ref));
+            const float g = __builtin_amdgcn_exp2f(s_m[k][col] * to2 - ref);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = __fmaf_rn(s_o[k][f / 4][4 * i + e][lane], g, x[e]);
         }

@@ -84,8 +84,8 @@ int rheo_cache_create(const rheo_cache_config* cfg, rheo_cache** out) {
     if (g.page_size < 1 || g.page_size > 4096 || (g.page_size & (g.page_size - 1)))
         return fail(RHEO_EINVAL, "page_size must be a power of two in [1, 4096]");
     if (g.pages < 1) return fail(RHEO_EINVAL, "pages must be >= 1");
-    if (g.table_width < 1 || (int64_t)g.table_width * g.page_size > 0x7FFFFFFF)
-        return fail(RHEO_EINVAL, "table_width must be >= 1 and a row's entries below 2^31");
+    if (g.table_width < 1 || (int64_t)g.table_width * g.page_size > (1 << 30))
+        return fail(RHEO_EINVAL, "table_width must be >= 1 and a row's entries at most 2^30");
     if (g.layers < 1 || g.layers > 1024) return fail(RHEO_EINVAL, "layers must be in [1, 1024]");
     if (g.dtype != RHEO_BF16 && g.dtype != RHEO_F16) return fail(RHEO_EINVAL, "unknown dtype");
     const int64_t page = (int64_t)g.page_size * g.kv_heads * g.head_dim;

@@ -115,14 +115,15 @@ __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
         } else {
             // the (room - 1 - v)-th returned page: the last sequence that fewer are
             // returned before (those that return none share their sum with the next)
-            const int r = (int)(room - 1 - v);
+            const int r = clamp31(room - 1 - v);
             int lo = 0, hi = B - 1;
             while (lo < hi) {
                 const int mid = (lo + hi + 1) >> 1;
                 if (s_give[mid] <= r) lo = mid; else hi = mid - 1;
             }
-            page = a.table[(int64_t)lo * c.width +
-                           min(max(s_need[lo], 0) + r - s_give[lo], c.width - 1)];
+            // (held out of range as a whole: sums that the index does not follow)
+            const int64_t at = (int64_t)max(s_need[lo], 0) + r - s_give[lo];
+            page = a.table[(int64_t)lo * c.width + (at < 0 ? 0 : at < c.width ? at : c.width - 1)];
         }
         if ((unsigned)page >= (unsigned)c.pages) {
             atomicOr(c.err, CE_PLAN);

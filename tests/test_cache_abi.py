@@ -16,7 +16,7 @@ BAD = [
     dict(batch=0), dict(batch=4097), dict(kv_heads=0), dict(heads=0), dict(heads=7),
     dict(heads=1032, kv_heads=8), dict(head_dim=0), dict(head_dim=12), dict(head_dim=264),
     dict(page_size=0), dict(page_size=24), dict(page_size=8192), dict(pages=0),
-    dict(table_width=0), dict(table_width=1 << 27), dict(layers=0), dict(layers=1025),
+    dict(table_width=0), dict(table_width=(1 << 26) + 1), dict(layers=0), dict(layers=1025),
     dict(dtype=0), dict(dtype=3), dict(page_stride=16 * 2 * 128 - 8), dict(page_stride=16 * 2 * 128 + 4),
     dict(page_stride=1 << 41), dict(layer_stride=1), dict(layer_stride=10 * 16 * 2 * 128 + 4),
     dict(layer_stride=9 * 16 * 2 * 128),

@@ -518,6 +518,13 @@ def test_attention_flags_pages_outside_the_pool(binding):
         c.attention(s.q.cuda(), s.kc.cuda(), s.vc.cuda(), s.table.clamp(min=0).cuda(), _i32([lens]))
         assert c.device_error() == 32
         c.close()
+    for count in (-1, 4):
+        c = binding.Cache(batch=1, heads=4, kv_heads=2, head_dim=64, page_size=16, pages=s.pages,
+                          table_width=s.width)
+        c.attention(s.q.cuda(), s.kc.cuda(), s.vc.cuda(), s.table.cuda(), _i32([70]),
+                    count=_i32([count]))
+        assert c.device_error() == 1
+        c.close()
     s.cache.close()
 
 
