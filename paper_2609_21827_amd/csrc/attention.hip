@@ -40,6 +40,7 @@ struct Shape {
     static constexpr int KW = NW / RT;               // waves to a row block
     static constexpr int KT = 32 * KW * U;           // entries of a tile
     static constexpr int ROWS = 32 * RT;
+    static constexpr bool DEAL = ROWS >= 128;        // see deal_items
     static constexpr int NT = 64 * NW;
     static constexpr int KS = DT / 16, DB = DT / 32; // steps of QK, blocks of O's columns
     static constexpr int ROWB = DT * 2;              // bytes of an LDS row
@@ -65,6 +66,7 @@ struct AttnArgs {
     int g;                         // query heads of a key head
     int groups;                    // most stretches (workgroups)
     int min_tiles;                 // fewest tiles of a stretch
+    int whole;                     // whole items may be given out (see deal_items)
     int* desc;                     // [groups][8]: what k_attn_join adds up
 };
 
@@ -114,6 +116,15 @@ __device__ __forceinline__ int64_t tiles_of_head(const AttnArgs& p, const Seq& s
     return t;
 }
 
+// What is the same in all lanes, said so: it then takes scalar registers.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform64(int64_t v) {
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+}
+__device__ __forceinline__ Seq uniform(const Seq& s) {
+    return Seq{uniform(s.len), uniform(s.rows), uniform(s.tail), uniform(s.nrb), uniform(s.entries)};
+}
+
 // Stretch w of the line: tiles [t0, t1) of it, the sequence that t0 is in and
 // the tiles before that sequence.  All threads of the block call it.
 struct Stretch {
@@ -145,6 +156,7 @@ __device__ Stretch find_stretch(const AttnArgs& p, int w) {
         if (v < wave) excl += s_wave[v];
         total += s_wave[v];
     }
+    total = uniform64(total);
     Stretch r;
     r.total = total;
     const int64_t most = (total + p.min_tiles - 1) / p.min_tiles;
@@ -168,9 +180,56 @@ __device__ Stretch find_stretch(const AttnArgs& p, int w) {
         }
     }
     __syncthreads();
-    r.seq = __builtin_amdgcn_readfirstlane(s_seq);
-    r.before = s_before;
+    r.seq = uniform(s_seq);
+    r.before = uniform64(s_before);
     return r;
+}
+
+// Whole items dealt out instead of stretches, where that is nearly as even: the
+// sequences sorted by length, their items given to the workgroups in order, there and
+// back (the longest with the shortest).  A cut costs the partial results' way out and
+// back, as long as some four tiles of 256 rows each, and the join: 64 trees of 244
+// rows over 1000 to 4096 entries 271 us in stretches, 237 dealt.  (Partial results
+// of 64 rows and fewer are too small for that: 3 % slower.)  All threads call it;
+// at most kDealt sequences, an item a key head each.
+constexpr int kDealt = 256;
+
+__device__ __forceinline__ int dealt_item(int round, int w, int groups) {
+    return round * groups + (round & 1 ? groups - 1 - w : w);
+}
+
+template <typename S>
+__device__ bool deal_items(const AttnArgs& p, int64_t total, int* s_order) {
+    __shared__ int s_tiles[kDealt], s_most[S::NW];
+    const int tid = threadIdx.x, B = p.c.B, K = p.c.K, items = B * K;
+    __syncthreads();
+    for (int b = tid; b < B; b += S::NT) {
+        const Seq s = seq_of<S>(p, b);
+        s_tiles[b] = s.nrb ? tiles_of<S>(p, s, 0) : 0;
+    }
+    __syncthreads();
+    for (int b = tid; b < B; b += S::NT) {
+        const int mine = s_tiles[b];
+        int rank = 0;
+        for (int o = 0; o < B; ++o) rank += s_tiles[o] > mine || (s_tiles[o] == mine && o < b);
+        s_order[rank] = b;
+    }
+    __syncthreads();
+    int most = 0;
+    for (int w = tid; w < p.groups; w += S::NT) {
+        int sum = 0;
+        for (int r = 0; r * p.groups < items; ++r) {
+            const int i = dealt_item(r, w, p.groups);
+            if (i < items) sum += s_tiles[s_order[i / K]];
+        }
+        most = max(most, sum);
+    }
+    for (int o = 32; o; o >>= 1) most = max(most, __shfl_xor(most, o));
+    if ((tid & 63) == 0) s_most[tid >> 6] = most;
+    __syncthreads();
+    for (int w = 0; w < S::NW; ++w) most = max(most, s_most[w]);
+    const int64_t mean = total / p.groups;
+    return most <= mean + mean / 16 + 4;
 }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -194,10 +253,12 @@ __device__ __forceinline__ f32x16 mfma(const u32x4& a, const u32x4& b, const f32
 // builtin would make every LDS read wait for all of them.)  No register is
 // written but m0, which nothing else here uses (the compiler reserves it).
 __device__ __forceinline__ void load_lds16(uint32_t lds, const void* p) {
+    lds = __builtin_amdgcn_readfirstlane(lds);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p)
                  : "memory");
 }
 __device__ __forceinline__ void load_lds4(uint32_t lds, const void* p) {
+    lds = __builtin_amdgcn_readfirstlane(lds);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(p)
                  : "memory");
 }
@@ -281,6 +342,7 @@ k_tree_attention(AttnArgs p) {
     extern __shared__ __align__(1024) char s_lds[];
     __shared__ float s_ml[S::KW > 1 ? S::NW * 64 : 2];
     __shared__ int s_bad;                            // values left out of the item's products
+    __shared__ int s_order[S::DEAL ? kDealt : 1];    // sequences, the longest first
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int rt = wave % S::RT, kw = wave / S::RT;
@@ -300,37 +362,59 @@ k_tree_attention(AttnArgs p) {
                      (lane & 1) * 8;
     if (tid == 0) s_bad = 0;
 
-    const Stretch st = find_stretch<S>(p, w);
-    if (st.t0 >= st.t1) {
+    Stretch st = find_stretch<S>(p, w);
+    bool dealt = false;
+    if constexpr (S::DEAL)
+        if (p.whole && st.groups == p.groups)
+            dealt = uniform(deal_items<S>(p, st.total, s_order)) != 0;
+    if (!dealt && st.t0 >= st.t1) {
         if (tid == 0) p.desc[8 * w] = 0;
         return;
     }
-    // the first item
-    int b = st.seq;
-    Seq sq = seq_of<S>(p, b);
-    int64_t rel = st.t0 - st.before;
-    const int64_t per_head = tiles_of_head<S>(p, sq);
-    int hk = (int)(rel / per_head), rb = 0;
-    rel -= hk * per_head;
-    while (rel >= tiles_of<S>(p, sq, rb)) rel -= tiles_of<S>(p, sq, rb++);
-    int tile = (int)rel;                                 // the item's tile to begin with
-    int64_t left = st.t1 - st.t0;
-    {
+    // the item at hand: sequence, key head, row block, its tile to begin with; the
+    // tiles left of the stretch, or the round of the deal
+    int b = 0, hk = 0, rb = 0, tile = 0, round = 0;
+    int64_t left = 0;
+    Seq sq;
+    auto next_dealt = [&]() {
+        for (; S::DEAL && round * p.groups < c.B * c.K; ++round) {
+            const int i = dealt_item(round, w, p.groups);
+            if (i >= c.B * c.K) continue;
+            b = uniform(s_order[i / c.K]);
+            hk = i % c.K;
+            sq = uniform(seq_of<S>(p, b));
+            if (sq.nrb) {
+                left = tiles_of<S>(p, sq, 0);
+                ++round;
+                return true;
+            }
+        }
+        return false;
+    };
+    if (tid == 0) p.desc[8 * w] = 0;
+    if (dealt) {
+        if (!next_dealt()) return;
+    } else {
+        b = st.seq;
+        sq = uniform(seq_of<S>(p, b));
+        int64_t rel = st.t0 - st.before;
+        const int64_t per_head = tiles_of_head<S>(p, sq);
+        hk = uniform((int)(rel / per_head));
+        rel -= hk * per_head;
+        while (rel >= tiles_of<S>(p, sq, rb)) rel -= tiles_of<S>(p, sq, rb++);
+        tile = (int)rel;
+        left = st.t1 - st.t0;
         // the join of the first item, by the first cut inside it
         const int64_t begins = st.t0 - tile, ends = begins + tiles_of<S>(p, sq, rb);
-        if (tid == 0) {
+        if (tid == 0 && tile > 0 && stretch_start(st.total, st.groups, w - 1) <= begins) {
             int* d = p.desc + 8 * w;
-            const bool mine = tile > 0 && stretch_start(st.total, st.groups, w - 1) <= begins;
-            d[0] = 0;
-            if (mine) {
-                int n = 2;
-                while (stretch_start(st.total, st.groups, w + n - 1) < ends) ++n;
-                d[0] = n;                            // partial results
-                d[1] = 2 * (w - 1) + (stretch_start(st.total, st.groups, w - 1) < begins ? 1 : 0);
-                d[2] = b;
-                d[3] = hk;
-                d[4] = rb;
-            }
+            int n = 2;
+            while (stretch_start(st.total, st.groups, w + n - 1) < ends) ++n;
+            d[0] = n;                                // partial results
+            d[1] = 2 * (w - 1) + (stretch_start(st.total, st.groups, w - 1) < begins ? 1 : 0);
+            d[2] = b;
+            d[3] = hk;
+            d[4] = rb;
         }
     }
 
@@ -627,12 +711,14 @@ k_tree_attention(AttnArgs p) {
         // the next item
         left -= end_tile - tile;
         tile = 0;
-        if (++rb == sq.nrb) {
+        if (dealt) {
+            if (!next_dealt()) break;
+        } else if (++rb == sq.nrb) {
             rb = 0;
             if (++hk == c.K) {
                 hk = 0;
                 if (left > 0) {
-                    do { sq = seq_of<S>(p, ++b); } while (sq.nrb == 0);
+                    do { sq = uniform(seq_of<S>(p, ++b)); } while (sq.nrb == 0);
                 }
             }
         }
@@ -796,6 +882,9 @@ hipError_t start(AttnArgs p, hipStream_t s) {
     static_assert(S::LDS <= 156 * 1024, "LDS");
     p.groups = p.c.slots * S::RESIDENT;
     p.min_tiles = 1;
+    // (fewer items than workgroups: the cuts are what fills them)
+    p.whole = (int64_t)p.a.n * p.g <= S::ROWS && p.c.B <= kDealt &&
+              (int64_t)p.c.B * p.c.K >= p.groups;
     k_tree_attention<T, S><<<p.groups, S::NT, S::LDS, s>>>(p);
     // Items that are cut once or twice take a wave a block of 32 elements, those of
     // which many stretches have a part eight waves

@@ -300,11 +300,11 @@ class Setup:
         assert self.cache.device_error() == 0
         return out.cpu(), lse.cpu()
 
-    def check(self, got, mask=None, count=None, scale=None):
+    def check(self, got, mask=None, count=None, scale=None, only=None):
         scale = self.D ** -0.5 if scale is None else scale
         count = [self.n] * self.B if count is None else count
         out, lse = got
-        for b in range(self.B):
+        for b in only or range(self.B):
             rows, tail = count[b], self.tail - (self.n - count[b])
             assert (out[b, rows:] == 9).all() and (lse[b, rows:] == 9).all()
             if not rows:
@@ -415,6 +415,36 @@ def test_attention_of_many_rows(binding, n):
     count = [n - 1, 77]
     s.check(s.run(mask, count), mask, count)
     s.cache.close()
+
+
+@pytest.mark.parametrize("B,n,H,K,D,lens", [
+    (70, 31, 16, 4, 64, "even"), (40, 61, 32, 8, 128, "even"), (40, 61, 32, 8, 128, "uneven"),
+    (256, 61, 4, 1, 64, "even"), (257, 61, 4, 1, 64, "even"), (90, 31, 32, 8, 64, "ragged"),
+    (70, 31, 16, 4, 160, "same")])
+def test_attention_of_many_sequences(binding, B, n, H, K, D, lens):
+    """More items than workgroups: given out whole where lengths even out, else in
+    stretches; sequences without rows among them."""
+    rng = random.Random(B + n)
+    lengths = [{"even": rng.randint(20, 300), "ragged": rng.randint(0, 90), "same": 77,
+                "uneven": 1500 if b == 3 else 10}[lens] for b in range(B)]
+    s = Setup(binding, BF16, lengths, n, n, H, K, D, 16, seed=B)
+    mask = _tree_mask(s.g, 1, n).expand(B, n, n).contiguous()
+    count = [rng.choice([0, 1, n, n]) for _ in range(B)] if lens == "ragged" else None
+    got = s.run(mask, count)
+    longest = max(range(B), key=lambda b: lengths[b])
+    only = {0, B - 1, longest, rng.randrange(B)}
+    s.check(got, mask, count, only=only)
+    # the others, against a run in the reversed order, which is given out otherwise: each is off
+    # the exact result by at most 2^-8 |o| + (2^-8 + small) sum p |v| with |v| below 6 here, so
+    # the two by twice that
+    back = list(reversed(range(B)))
+    t = Setup(binding, BF16, lengths, n, n, H, K, D, 16, seed=B)
+    t.lens, t.q, t.table = [lengths[b] for b in back], s.q[back], s.table[back]
+    again = t.run(mask, None if count is None else [count[b] for b in back])
+    off = (again[0][back].float() - got[0].float()).abs()
+    assert float(s.vc.float().abs().max()) < 6
+    assert (off <= 2 * 2.0 ** -8 * (got[0].float().abs() + 1.1 * 6)).all()
+    s.cache.close(), t.cache.close()
 
 
 @pytest.mark.parametrize("dtype,n,H,K,D", [(BF16, 61, 8, 2, 128), (F16, 61, 4, 4, 128),
