@@ -154,6 +154,10 @@ __device__ __forceinline__ void put_outputs(const LogprobArgs& a, int entry, con
 // rise) is looked at again with its top-th largest key, found bit by bit over
 // the registers: at most `top` are that large.
 //
+// 640 rows of 151936 bf16 (194 MB, 41 us at the copy's rate): 45 us without
+// alternatives, 77 with 20, most of the difference in the first chunks' bounds and
+// ranks.  Half of a wave's time is waits there, a fifth issue.
+//
 template <int DT>
 __global__ __launch_bounds__(NTL) void k_row_stats(ScoreDev c, LogprobArgs a, int segs,
                                                    int seg_chunks) {
