@@ -331,6 +331,44 @@ def test_results_do_not_depend_on_earlier_calls(binding):
     s.cache.close()
 
 
+def test_entries_past_32_bits_of_offset(binding):
+    """A pool of 5 GiB of keys: pages at its end, behind 2^32 bytes and 2^31 elements, written,
+    attended and moved as the same entries of a small pool are."""
+    B, n, H, K, D, page, depth = 1, 20, 8, 8, 128, 64, 5
+    far, near = 41000, 4
+    g = torch.Generator().manual_seed(0)
+    q, k, v = ((torch.randn((B, n, h, D), generator=g)).to(BF16).cuda() for h in (H, K, K))
+    old = [torch.randn((near, page, K, D), generator=g).to(BF16).cuda() for _ in range(2)]
+    mask = _tree_mask(g, B, n).cuda()
+    parent = _i32([[-1] + [i - 1 for i in range(1, n)]])
+    token = _i32([[-1] + list(range(1, n))])
+    lens, took = _i32([3 * page - 7]), _i32([3])
+    accepted = _i32([[1, 2, 3, -1, -1]])
+    parent[0, 1:4] = torch.tensor([0, 4, 9], dtype=torch.int32)      # 0 -> 4 -> 9 -> 15
+    parent[0, 4], parent[0, 9], parent[0, 15] = 0, 4, 9
+    token[0, 4], token[0, 9], token[0, 15] = 101, 102, 103
+    accepted[0, :3] = torch.tensor([101, 102, 103], dtype=torch.int32)
+    got = []
+    for pages, first in ((near, 0), (far, far - near)):
+        c = binding.Cache(batch=B, heads=H, kv_heads=K, head_dim=D, page_size=page, pages=pages,
+                          table_width=near)
+        pools = [torch.empty((1, pages, page, K, D), dtype=BF16, device="cuda") for _ in range(2)]
+        for pool, x in zip(pools, old):
+            pool[0, first:] = x
+        table = _i32([[first + i for i in (2, 0, 3, 1)]])
+        e = torch.arange(n, device="cuda") + int(lens)
+        slots = (table[0].long()[e // page] * page + e % page)[None]
+        c.write(q, k, v, slots, pools[0][0], pools[1][0])
+        out, lse = c.attention(q, pools[0][0], pools[1][0], table, lens, mask=mask, lse=True)
+        path, new = c.commit(parent, token, accepted, took, lens, table, *pools)
+        assert c.device_error() == 0
+        got.append([out, lse, path, new] + [pool[0, first:].clone() for pool in pools])
+        c.close()
+        del pools
+    assert got[0][2].tolist() == [[0, 4, 9, 15, -1, -1]]
+    _same(*got)
+
+
 # -- whole decoding steps -----------------------------------------------------------------
 
 
