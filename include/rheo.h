@@ -442,7 +442,8 @@ typedef struct rheo_scorer rheo_scorer;
 
 /* A scorer of logit rows of `vocab` elements (2 <= vocab <= 2^24), row_stride
  * elements apart (conventions as for logit rows above; RHEO_F32, RHEO_BF16 or
- * RHEO_F16).  It owns a workspace of fixed size. */
+ * RHEO_F16).  It owns a workspace of fixed size; creation synchronises the
+ * device. */
 int rheo_scorer_create(int32_t vocab, int32_t dtype, int64_t row_stride, rheo_scorer** out);
 int rheo_scorer_destroy(rheo_scorer* scorer);
 

@@ -267,9 +267,12 @@ int rheo_scorer_create(int32_t vocab, int32_t dtype, int64_t row_stride, rheo_sc
     rheo_scorer* s = new (std::nothrow) rheo_scorer();
     if (!s) return fail(RHEO_ENOMEM, "out of host memory");
     s->dev = ScoreDev{vocab, dtype, row_stride, nullptr};
-    const hipError_t e = hipGetDevice(&s->device);
+    hipError_t e = hipGetDevice(&s->device);
     int rc = e == hipSuccess ? RHEO_OK : hip_fail(e, "hipGetDevice");
     if (rc == RHEO_OK) rc = zeroed((void**)&s->dev.work, score_workspace());
+    // (the fill must not land in a first call's results on another stream)
+    if (rc == RHEO_OK && (e = hipDeviceSynchronize()) != hipSuccess)
+        rc = hip_fail(e, "initialising a workspace");
     if (rc != RHEO_OK) {
         if (s->dev.work) (void)hipFree(s->dev.work);
         delete s;

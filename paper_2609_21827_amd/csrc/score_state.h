@@ -9,7 +9,7 @@ namespace rheo {
 struct ScoreDev {
     int V, dtype;
     int64_t stride;
-    char* work;                    // partial results of split rows (kScoreWork bytes)
+    char* work;                    // partial results of split rows (score_workspace() bytes)
 };
 
 struct LogprobArgs {

@@ -132,3 +132,25 @@ def test_one_sure_token(binding):
     assert logp.item() == 0 and ent.item() == 0 and rank.item() == 0
     assert ids.tolist() == [[[77, 0]]] and lps[0, 0].tolist() == [0.0, -math.inf]
     s.close()
+
+
+def test_a_new_scorer_used_at_once_on_another_stream(binding):
+    """Its workspace is filled behind work of the default stream, which the other stream
+    does not wait for: creation has to."""
+    g = torch.Generator().manual_seed(3)
+    x = _rows(g, 1, 2, 50000, BF16).cuda()
+    tokens = torch.tensor([[11, 49999]], dtype=torch.int32, device="cuda")
+    old = binding.Scorer(50000, BF16)
+    want = old.logprobs(x, tokens, top=20)
+    big = torch.ones((4096, 4096), device="cuda")
+    side = torch.cuda.Stream()
+    out = tuple(torch.zeros_like(t) for t in want)
+    torch.cuda.synchronize()
+    for _ in range(10):
+        big = big @ big * 2.0 ** -12
+    s = binding.Scorer(50000, BF16)
+    s.logprobs(x, tokens, top=20, out=out, stream=side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
+    s.close()
+    old.close()
