@@ -327,7 +327,7 @@ int rheo_cache_destroy(rheo_cache* cache);
  * lens, count, held, free_count or the free list out of range in
  * rheo_cache_plan, count in rheo_tree_attention; bit 1: a slot >= pages * page_size; bit 2: a position
  * outside the rotation table; bit 3: a page outside the pool; bit 4: an
- * accepted token that is no child of the node before it; bit 5: entries
+ * accepted token that is no child, at a higher index, of the node before it; bit 5: entries
  * past the table's row. */
 int rheo_cache_error(rheo_cache* cache, int32_t* host_flag);
 

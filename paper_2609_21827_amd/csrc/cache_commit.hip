@@ -52,10 +52,12 @@ __global__ __launch_bounds__(NTC) void k_cache_commit(CacheDev c, CommitArgs a, 
                 int found = 0;
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const uint64_t m = __ballot(par[k] == node && tok[k] == want);
+                    const uint64_t m = __ballot(par[k] == node && tok[k] == want &&
+                                                64 * k + lane > node);
                     if (m && !found) found = 64 * k + __builtin_ctzll(m);
                 }
-                // (children come behind their parents, so the search starts there)
+                // (children come behind their parents; only those count, in whatever
+                // tree, so that the path rises as the moves need it)
                 for (int i0 = max(node + 1, 128); i0 < a.n && !found; i0 += 64) {
                     const int i = i0 + lane;
                     const bool hit = i < a.n && parent[i] == node && token[i] == want;

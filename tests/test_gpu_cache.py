@@ -651,3 +651,18 @@ def test_commit_flags_bad_data(binding, kw, bit):
     assert path.tolist() == [[-1, -1, -1]] and new.tolist() == base["lens"]
     assert torch.equal(kc, k0) and torch.equal(vc, k0)
     c.close()
+
+
+@pytest.mark.parametrize("parent,accepted", [([-1, 2, 0, 1], [5, 4]), ([-1, 3, 0, 0], [6, 4])])
+def test_commit_of_children_ahead_of_their_parents_is_flagged(binding, parent, accepted):
+    """No tree has them, and moves along such a path would read what they have written."""
+    kc = torch.randn((1, 4, 32, 1, 64), device="cuda").to(BF16)
+    vc, k0 = kc.clone(), kc.clone()
+    c = binding.Cache(batch=1, heads=1, kv_heads=1, head_dim=64, page_size=32, pages=4,
+                      table_width=4)
+    path, new = c.commit(_i32([parent]), _i32([[-1, 4, 5, 6]]), _i32([accepted]), _i32([2]),
+                         _i32([33]), _i32([[0, 1, 2, 3]]), kc, vc)
+    assert c.device_error() == 16
+    assert path.tolist() == [[-1, -1, -1]] and new.tolist() == [33]
+    assert torch.equal(kc, k0) and torch.equal(vc, k0)
+    c.close()
