@@ -404,7 +404,7 @@ typedef struct rheo_attention_args {
                                     behind the prefix                                 */
     const uint8_t* mask;         /* [B][n][tail], row i attends entry lens[b] + j iff
                                     not 0; NULL: iff j <= i + tail - n                  */
-    float scale;                 /* > 0                                                 */
+    float scale;                 /* 2^-100..2^100                                       */
     void* out;                   /* as q; not q itself                                  */
     float* lse;                  /* [B * n][heads] or NULL: log of the sum of
                                     exp(scale q.k) over what the row attends            */

@@ -214,8 +214,9 @@ int rheo_tree_attention(rheo_cache* c, const rheo_attention_args* args, void* st
     // (a tail of 2^24 entries: its masks' rows stay within 32 bits of each other)
     if (a.tail < 0 || a.tail > (1 << 24)) return fail(RHEO_EINVAL, "tail must be in [0, 2^24]");
     if (!a.mask && a.tail < a.n) return fail(RHEO_EINVAL, "tail must be >= n without a mask");
-    if (!(a.scale > 0.0f) || !std::isfinite(a.scale))
-        return fail(RHEO_EINVAL, "scale must be finite and > 0");
+    // (8 / scale, the slack of the kernel's reference, and scale log2(e) stay finite)
+    if (!(a.scale >= 0x1p-100f && a.scale <= 0x1p100f))
+        return fail(RHEO_EINVAL, "scale must be in [2^-100, 2^100]");
     if (a.n == 0) return RHEO_OK;            // (empty arrays may have no address)
     if ((rc = check_ptr(a.q, "q")) || (rc = check_ptr(a.out, "out"))) return rc;
     if ((rc = check_stride(a.q_stride, (int64_t)d.H * d.D, "q_stride"))) return rc;

@@ -493,3 +493,20 @@ def test_decoding_steps_with_a_model(binding):
     assert accepted_any > 0
     assert cache.device_error() == 0 and tree.device_error() == 0
     tree.close(), cache.close(), scorer.close()
+
+
+def test_smallest_scale_and_scales_out_of_range(binding):
+    """2^-100: all weights are the same.  A scale so small that 8 / scale is infinite would
+    leave the running maximum where it began, and is refused."""
+    s = Setup(binding, BF16, [40], 3, 3, 4, 2, 64, 16)
+    q = s.q.cuda()
+    kc, vc = s.pages_on_gpu()
+    table, lens = s.table.cuda(), _i32(s.lens)
+    _, lse = s.cache.attention(q, kc, vc, table, lens, scale=2.0 ** -100, lse=True)
+    want = torch.tensor([41.0, 42.0, 43.0]).double().log()
+    # 43 terms of 1 are exact; their logarithm and its sum with 0: some roundings
+    assert ((lse.cpu().double() - want[None, :, None]).abs() <= 8 * 2.0 ** -24 * 4).all()
+    for bad in (2.0 ** -101, 1e-38, 2.0 ** 101, 3e38, 0.0, -1.0, float("inf"), float("nan")):
+        with pytest.raises(binding.RheoError):
+            s.cache.attention(q, kc, vc, table, lens, scale=bad)
+    s.cache.close()
