@@ -313,7 +313,8 @@ typedef struct rheo_cache_config {
                                     page_size <= 2^30                                 */
     int32_t layers;              /* layers one rheo_cache_commit moves, 1..1024          */
     int32_t dtype;               /* RHEO_BF16 or RHEO_F16                               */
-    int64_t page_stride;         /* >= page_size * kv_heads * head_dim; 0: equal to it   */
+    int64_t page_stride;         /* >= page_size * kv_heads * head_dim; 0: equal to it;
+                                    pages * page_stride <= 2^48                       */
     int64_t layer_stride;        /* >= pages * page_stride; 0: equal to it               */
 } rheo_cache_config;
 

@@ -92,6 +92,9 @@ int rheo_cache_create(const rheo_cache_config* cfg, rheo_cache** out) {
     const int64_t page_stride = g.page_stride ? g.page_stride : page;
     if (page_stride < page || page_stride % 8 || page_stride > ((int64_t)1 << 40))
         return fail(RHEO_EINVAL, "page_stride must hold a page and be a multiple of 16 bytes");
+    // (byte offsets of a pool's entries stay within 64 bits)
+    if (page_stride > ((int64_t)1 << 48) / g.pages)
+        return fail(RHEO_EINVAL, "pages * page_stride must be at most 2^48");
     // (the last page need not be followed by a gap)
     const int64_t layer = (g.pages - 1) * page_stride + page;
     const int64_t layer_stride = g.layer_stride ? g.layer_stride : g.pages * page_stride;

@@ -72,3 +72,13 @@ def test_trees_keep_their_types():
     cfg = binding.RheoConfig(2, 1000, 4, 1, 3, 0, 128, 0, binding.RHEO_F16, 0, 0, 1000, 0.0)
     h = ctypes.c_void_p()
     assert lib.rheo_create(ctypes.byref(cfg), ctypes.byref(h)) == binding.RHEO_EINVAL
+
+
+@needs_lib
+@pytest.mark.parametrize("bad", [dict(pages=2 ** 31 - 1, page_stride=1 << 40, layers=1),
+                                 dict(pages=2 ** 31 - 1, page_stride=1 << 33, layers=2),
+                                 dict(pages=257, page_stride=1 << 40, layers=1)])
+def test_pools_past_64_bits_are_refused(bad):
+    test_invalid_cache_configs_are_refused(bad)
+    from paper_2609_21827_amd import binding
+    assert "2^48" in binding.load_library().rheo_last_error().decode()
