@@ -326,10 +326,10 @@ int rheo_cache_destroy(rheo_cache* cache);
 
 /* Synchronises the handle's device and reads its sticky error flag: bit 0:
  * lens, count, held, free_count or the free list out of range in
- * rheo_cache_plan, count in rheo_tree_attention; bit 1: a slot >= pages * page_size; bit 2: a position
- * outside the rotation table; bit 3: a page outside the pool; bit 4: an
- * accepted token that is no child, at a higher index, of the node before it; bit 5: entries
- * past the table's row. */
+ * rheo_cache_plan, count in rheo_tree_attention; bit 1: a slot >= pages *
+ * page_size; bit 2: a position outside the rotation table; bit 3: a page
+ * outside the pool; bit 4: an accepted token that is no child, at a higher
+ * index, of the node before it; bit 5: entries past the table's row. */
 int rheo_cache_error(rheo_cache* cache, int32_t* host_flag);
 
 /* Pages and slots for the next rows of every sequence.
@@ -388,7 +388,7 @@ typedef struct rheo_write_args {
  * position ((a, b) -> (a cos - b sin, b cos + a sin)); q goes to q_out, k
  * and v to the row's slot.  fp32 inside, one rounding at the end.  Slots of one
  * call are distinct (else which row stays is undefined); q, k and v do not
- * overlap the pages. */
+ * overlap the pages, and q_out, unless it is q, none of them. */
 int rheo_cache_write(rheo_cache* cache, const rheo_write_args* args, void* stream);
 
 typedef struct rheo_attention_args {
@@ -406,7 +406,7 @@ typedef struct rheo_attention_args {
     const uint8_t* mask;         /* [B][n][tail], row i attends entry lens[b] + j iff
                                     not 0; NULL: iff j <= i + tail - n                  */
     float scale;                 /* 2^-100..2^100                                       */
-    void* out;                   /* as q; not q itself                                  */
+    void* out;                   /* as q; overlaps neither q nor the pages               */
     float* lse;                  /* [B * n][heads] or NULL: log of the sum of
                                     exp(scale q.k) over what the row attends            */
 } rheo_attention_args;
@@ -417,7 +417,7 @@ typedef struct rheo_attention_args {
  * accumulators; the probabilities enter the second product in cfg.dtype.  A row
  * that attends nothing gives 0 and lse -inf.  Rows i >= count[b] are left as
  * they were.  What a row does not attend has no effect on it, whatever it
- * holds. */
+ * holds; keys that it does attend are finite (else its output may be NaN). */
 int rheo_tree_attention(rheo_cache* cache, const rheo_attention_args* args, void* stream);
 
 /* Keeps the accepted path of a verified tree: with parent and token [B][n] as

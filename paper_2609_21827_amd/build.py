@@ -47,10 +47,13 @@ def _compile(out, sources, verbose, jobs=None):
     """One object per source, `jobs` compilers at a time, then the library."""
     objs = [os.path.join(HERE, "build", os.path.basename(out) + "." + s + ".o") for s in sources]
     os.makedirs(os.path.join(HERE, "build"), exist_ok=True)
+
+    def one(source, obj):
+        _run([HIPCC] + FLAGS + SOURCE_FLAGS.get(source, []) +
+             ["-c", os.path.join(CSRC, source), "-o", obj], verbose)
+
     with ThreadPoolExecutor(jobs or min(4, os.cpu_count() or 1)) as pool:
-        list(pool.map(lambda so: _run([HIPCC] + FLAGS + SOURCE_FLAGS.get(so[0], []) + ["-c", os.path.join(CSRC, so[0]),
-                                                         "-o", so[1]], verbose),
-                      zip(sources, objs)))
+        list(pool.map(one, sources, objs))
     _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", out + ".tmp"] + objs, verbose)
     os.replace(out + ".tmp", out)
     return out
