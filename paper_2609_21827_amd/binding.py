@@ -284,7 +284,8 @@ def _refuse(msg):
 class _OnDevice:
     """What the handles below share: tensors are checked for place, type, shape and
     layout (nothing is copied or converted), outputs are allocated on the handle's
-    device, and a stream given by the caller is noted with the allocator.
+    device, in the order of the stream that the call runs on, and a stream given by
+    the caller is noted with the allocator.
 
     A call is some 5 us of checks and marshalling beside kernels of 4 us, so the
     checks are few and plain: get_device() and `is` instead of device and dtype
@@ -308,10 +309,25 @@ class _OnDevice:
             _refuse(f"{name} must be contiguous")
         return t.data_ptr()
 
-    def _made(self, t, dtype, shape, name):
+    def _new(self, dtype, shape, stream, make=torch.empty):
+        """A new output of a call on `stream`.
+
+        Memory comes back to the allocator while the stream that it was made on has still
+        work on it to do, and a fill is work of its own: both are in order only for
+        calls on that very stream.  So the output is made on the call's stream, and
+        torch's current stream, where the caller reads it, is noted with it."""
+        if stream is None or stream.cuda_stream == _current_stream(self._index):
+            return make(shape, dtype=dtype, device=self.device)
+        reader = torch.cuda.current_stream(self._index)
+        with torch.cuda.stream(stream):
+            t = make(shape, dtype=dtype, device=self.device)
+        t.record_stream(reader)
+        return t
+
+    def _made(self, t, dtype, shape, name, stream):
         """(tensor, address) of an output, allocated unless given."""
         if t is None:
-            t = torch.empty(shape, dtype=dtype, device=self.device)
+            t = self._new(dtype, shape, stream)
             return t, t.data_ptr()
         return t, self._dense(t, dtype, shape, name)
 
@@ -405,9 +421,9 @@ class Cache(_OnDevice):
         B, i32 = self.B, self._i32
         one, rows = (B,), (B, n)
         slots, positions, status = out or (None, None, None)
-        slots, p_slots = self._made(slots, torch.int64, rows, "slots")
-        positions, p_positions = self._made(positions, torch.int32, rows, "positions")
-        status, p_status = self._made(status, torch.int32, one, "status")
+        slots, p_slots = self._made(slots, torch.int64, rows, "slots", stream)
+        positions, p_positions = self._made(positions, torch.int32, rows, "positions", stream)
+        status, p_status = self._made(status, torch.int32, one, "status", stream)
         _check(_LIB.rheo_cache_plan(
             self._h, n, i32(lens, one, "lens"), i32(count, one, "count"), i32(depth, rows, "depth"),
             i32(held, one, "held"), i32(table, (B, self.width), "table"),
@@ -429,7 +445,7 @@ class Cache(_OnDevice):
         if q is not None:
             p_q, q_row = self._rows(q, n, self.H, "q")
             if out is None:
-                out = torch.empty((B, n, self.H, self.D), dtype=self.dtype, device=self.device)
+                out = self._new(self.dtype, (B, n, self.H, self.D), stream)
             p_out, out_row = self._rows(out, n, self.H, "out")
         elif out is not None:
             _refuse("out without q")
@@ -470,12 +486,12 @@ class Cache(_OnDevice):
         if mask is not None:         # (one without columns has no address, but names nothing)
             p_mask = self._dense(mask, torch.uint8, (B, n, tail), "mask") or p_table
         if out is None:
-            out = torch.empty((B, n, self.H, self.D), dtype=self.dtype, device=self.device)
+            out = self._new(self.dtype, (B, n, self.H, self.D), stream)
         p_out, out_row = self._rows(out, n, self.H, "out")
         both, p_lse = lse is not None and lse is not False, None
         if both:
             lse, p_lse = self._made(None if lse is True else lse, torch.float32, (B, n, self.H),
-                                    "lse")
+                                    "lse", stream)
         a = AttentionArgs(
             n, tail, p_q, q_row, out_row, self._pages(k_cache, "k_cache"),
             self._pages(v_cache, "v_cache"), p_table, self._i32(lens, (B,), "lens"),
@@ -494,8 +510,8 @@ class Cache(_OnDevice):
         B, n, depth, i32 = self.B, parent.shape[-1], accepted.shape[-1], self._i32
         one, rows = (B,), (B, n)
         path, new_lens = out or (None, None)
-        path, p_path = self._made(path, torch.int32, (B, depth + 1), "path")
-        new_lens, p_new = self._made(new_lens, torch.int32, one, "new_lens")
+        path, p_path = self._made(path, torch.int32, (B, depth + 1), "path", stream)
+        new_lens, p_new = self._made(new_lens, torch.int32, one, "new_lens", stream)
         _check(_LIB.rheo_cache_commit(
             self._h, n, depth, i32(parent, rows, "parent"), i32(token, rows, "token"),
             i32(accepted, (B, depth), "accepted"), i32(accept_len, one, "accept_len"),
@@ -539,7 +555,7 @@ class Scorer(_OnDevice):
                 ("rank", torch.int32, one), ("top_token", torch.int32, best),
                 ("top_logprob", torch.float32, best))
         if out is None:
-            out = tuple(torch.zeros(s, dtype=d, device=self.device) for _, d, s in want)
+            out = tuple(self._new(d, s, stream, torch.zeros) for _, d, s in want)
         if len(out) != len(want):
             _refuse(f"out must be {len(want)} tensors")
         _check(_LIB.rheo_token_logprobs(
