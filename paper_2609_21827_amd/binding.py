@@ -309,6 +309,15 @@ class _OnDevice:
             _refuse(f"{name} must be contiguous")
         return t.data_ptr()
 
+    def _aside(self, stream):
+        """Whether a stream is another than torch's current one; it has to be of the
+        handle's device, since its outputs are made and its kernels run there."""
+        if stream is None:
+            return False
+        if stream.device_index != self._index:
+            _refuse(f"stream must be of {self.device}, got one of device {stream.device_index}")
+        return stream.cuda_stream != _current_stream(self._index)
+
     def _new(self, dtype, shape, stream, make=torch.empty):
         """A new output of a call on `stream`.
 
@@ -316,7 +325,7 @@ class _OnDevice:
         work on it to do, and a fill is work of its own: both are in order only for
         calls on that very stream.  So the output is made on the call's stream, and
         torch's current stream, where the caller reads it, is noted with it."""
-        if stream is None or stream.cuda_stream == _current_stream(self._index):
+        if not self._aside(stream):
             return make(shape, dtype=dtype, device=self.device)
         reader = torch.cuda.current_stream(self._index)
         with torch.cuda.stream(stream):
@@ -336,7 +345,7 @@ class _OnDevice:
         tensors, so that their memory is not used again before its work has run."""
         if stream is None:
             return _current_stream(self._index)
-        if stream.cuda_stream != _current_stream(self._index):
+        if self._aside(stream):
             for t in tensors:
                 if t is not None:
                     t.record_stream(stream)

@@ -106,3 +106,18 @@ def test_they_are_not_handed_out_again_while_the_current_stream_reads_them(bindi
     assert len(again) == 3
     for h in handles:
         h.close()
+
+
+def test_streams_of_other_libraries(binding):
+    """A stream known by its address alone."""
+    calls, handles = _calls(binding)
+    side = torch.cuda.Stream()
+    for name in NAMES:
+        want = [t.clone() for t in calls[name](0, None)]
+        torch.cuda.synchronize()
+        got = calls[name](0, torch.cuda.ExternalStream(side.cuda_stream))
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert torch.equal(x, y)
+    for h in handles:
+        h.close()
