@@ -593,14 +593,16 @@ k_tree_attention(AttnArgs p) {
                 for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[u][i]);
             const f32x2 mb = both_halves(mx);
             const float m = fmaxf(x.m, fmaxf(mb[0], mb[1]));
-            if (__any(m > x.m + slack)) {
-                // (both references as the exponents have them, rounded)
-                const float f = __builtin_amdgcn_exp2f(
-                    x.m * to2 - (m == -INFINITY ? 0.0f : m * to2));
+            const bool up = m > x.m + slack;
+            if (__any(up)) {
+                // (both references as the exponents have them, rounded; a row whose own
+                // maximum has not risen so far keeps its reference, so that what other rows
+                // attend does not show in its roundings)
+                const float f = up ? __builtin_amdgcn_exp2f(x.m * to2 - m * to2) : 1.0f;
                 x.l *= f;
 #pragma unroll
                 for (int d = 0; d < S::DB; ++d) x.o[d] *= f;
-                x.m = m;
+                x.m = up ? m : x.m;
             }
             const float ref = x.m == -INFINITY ? 0.0f : x.m * to2;
             float sum = 0.0f;
