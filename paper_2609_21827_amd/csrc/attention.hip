@@ -335,6 +335,30 @@ __device__ __forceinline__ void add_unfinite(const AttnArgs& p, int b, int hk, c
     }
 }
 
+// The exponents' reference stands at most kSlack<T> below a row's largest score so far (in
+// units of log2), and kRise<T> lower still: a probability is at most 2^15 as it enters the
+// second product.  For bf16, which has fp32's exponents, that is 2^8 and no rise.  fp16
+// ends at 65504 and has full accuracy from 2^-14 on, so its probabilities take all of the
+// upper range: those down to 2^-25 (17 nats) of the largest are rounded to 11 bits, and
+// 2^-36 of it is the most that smaller ones are off by.  (With the largest at 1, keys 17
+// nats below a sink lost 44 % of their weight to the smallest step.)
+template <typename T>
+constexpr float kSlack = std::is_same<T, __bf16>::value ? 8.0f : 4.0f;
+template <typename T>
+constexpr float kRise = std::is_same<T, __bf16>::value ? 0.0f : 11.0f;
+
+// The reference as the exponents have it, rounded; any where a row has no score yet.
+template <typename T>
+__device__ __forceinline__ float ref_of(float m, float to2) {
+    return m == -INFINITY ? 0.0f : m * to2 - kRise<T>;
+}
+// ln of a sum relative to it
+template <typename T>
+__device__ __forceinline__ float lse_of(float m, float l, float scale) {
+    constexpr float down = std::is_same<T, __bf16>::value ? 1.0f : 0x1p-11f;    // 2^-kRise, exact
+    return m * scale + logf(l * down);
+}
+
 // What a row block's waves hold while they go through an item's tiles.
 template <typename S>
 struct Rows {
@@ -359,7 +383,7 @@ k_tree_attention(AttnArgs p) {
     const rheo_attention_args& a = p.a;
     const int w = blockIdx.x, D = c.D;
     const float to2 = a.scale * kLog2e;              // scores to exponents of 2
-    const float slack = 8.0f / to2;
+    const float slack = kSlack<T> / to2;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_lds;
     const uint32_t lds_mine = __builtin_amdgcn_readfirstlane(lds0 + wave * (S::J * 1024));
     const uint32_t lds_pages = __builtin_amdgcn_readfirstlane(lds0 + S::RING + wave * 256);
@@ -582,10 +606,9 @@ k_tree_attention(AttnArgs p) {
                             sc[u][i] = eh + u * 32 + 8 * (i / 4) + i % 4 < end ? sc[u][i] : -INFINITY;
                 }
             }
-            // The exponents' reference is the row's maximum so far, or lower by up to 8:
-            // probabilities are then at most 2^8, which all that holds them takes, and
-            // O is rescaled once or twice an item instead of at most tiles (some row of
-            // 32 has a new maximum).
+            // The exponents' reference follows the row's maximum by steps (kSlack): what holds
+            // the probabilities takes them, and O is rescaled once or twice an item instead
+            // of at most tiles (some row of 32 has a new maximum).
             float mx = sc[0][0];
 #pragma unroll
             for (int u = 0; u < S::U; ++u)
@@ -598,13 +621,14 @@ k_tree_attention(AttnArgs p) {
                 // (both references as the exponents have them, rounded; a row whose own
                 // maximum has not risen so far keeps its reference, so that what other rows
                 // attend does not show in its roundings)
-                const float f = up ? __builtin_amdgcn_exp2f(x.m * to2 - m * to2) : 1.0f;
+                const float f =
+                    up ? __builtin_amdgcn_exp2f((x.m * to2 - kRise<T>) - ref_of<T>(m, to2)) : 1.0f;
                 x.l *= f;
 #pragma unroll
                 for (int d = 0; d < S::DB; ++d) x.o[d] *= f;
                 x.m = up ? m : x.m;
             }
-            const float ref = x.m == -INFINITY ? 0.0f : x.m * to2;
+            const float ref = ref_of<T>(x.m, to2);
             float sum = 0.0f;
 #pragma unroll
             for (int u = 0; u < S::U; ++u)
@@ -655,13 +679,13 @@ k_tree_attention(AttnArgs p) {
             float m = -INFINITY, l = 0.0f;
 #pragma unroll
             for (int k = 0; k < S::KW; ++k) m = fmaxf(m, s_ml[((k * S::RT + rt) * 32 + col) * 2]);
-            const float ref = m == -INFINITY ? 0.0f : m * to2;
+            const float ref = ref_of<T>(m, to2);
 #pragma unroll
             for (int k = 0; k < S::KW; ++k) {
                 const float* ml = s_ml + ((k * S::RT + rt) * 32 + col) * 2;
-                l += ml[1] * __builtin_amdgcn_exp2f(ml[0] * to2 - ref);
+                l += ml[1] * __builtin_amdgcn_exp2f((ml[0] * to2 - kRise<T>) - ref);
             }
-            const float f = __builtin_amdgcn_exp2f(x.m * to2 - ref);
+            const float f = __builtin_amdgcn_exp2f((x.m * to2 - kRise<T>) - ref);
             float* out = (float*)s_lds;
 #pragma unroll
             for (int d = 0; d < S::DB; ++d) {
@@ -701,7 +725,7 @@ k_tree_attention(AttnArgs p) {
                                     pack2<T>(x.o[d][4 * i] * inv, x.o[d][4 * i + 1] * inv),
                                     pack2<T>(x.o[d][4 * i + 2] * inv, x.o[d][4 * i + 3] * inv));
                         }
-                    if (a.lse && !half) a.lse[qrow * c.H + qh] = x.m * a.scale + logf(x.l);
+                    if (a.lse && !half) a.lse[qrow * c.H + qh] = lse_of<T>(x.m, x.l, a.scale);
                     if (bad) add_unfinite<T>(p, b, hk, sq, qi, o, 4 * half, 8);
                 }
             } else {
@@ -784,10 +808,10 @@ __global__ __launch_bounds__(NTJ) void k_attn_join(AttnArgs p) {
         const float m0 = q0[ml], l0 = q0[ml + 1];
         const float m1 = k + NS < n ? q1[ml] : -INFINITY, l1 = q1[ml + 1];
         bad |= ((const int*)q0)[S::PART - 1] | ((const int*)q1)[S::PART - 1];
-        const float top = fmaxf(m, fmaxf(m0, m1)), ref = top == -INFINITY ? 0.0f : top * to2;
-        const float f = __builtin_amdgcn_exp2f(m * to2 - ref);
-        const float g0 = __builtin_amdgcn_exp2f(m0 * to2 - ref);
-        const float g1 = __builtin_amdgcn_exp2f(m1 * to2 - ref);
+        const float top = fmaxf(m, fmaxf(m0, m1)), ref = ref_of<T>(top, to2);
+        const float f = __builtin_amdgcn_exp2f((m * to2 - kRise<T>) - ref);
+        const float g0 = __builtin_amdgcn_exp2f((m0 * to2 - kRise<T>) - ref);
+        const float g1 = __builtin_amdgcn_exp2f((m1 * to2 - kRise<T>) - ref);
         m = top;
         l = l * f + l0 * g0;
         if (k + NS < n) l = __fmaf_rn(l1, g1, l);
@@ -812,11 +836,11 @@ __global__ __launch_bounds__(NTJ) void k_attn_join(AttnArgs p) {
     const int parts = min(n, NS), r = rb * S::ROWS + rt * 32 + col;
     m = -INFINITY;
     for (int k = 0; k < parts; ++k) m = fmaxf(m, s_m[k][col]);
-    const float ref = m == -INFINITY ? 0.0f : m * to2;
+    const float ref = ref_of<T>(m, to2);
     l = 0.0f;
     bad = 0;
     for (int k = 0; k < parts; ++k) {
-        l = __fmaf_rn(s_l[k][col], __builtin_amdgcn_exp2f(s_m[k][col] * to2 - ref), l);
+        l = __fmaf_rn(s_l[k][col], __builtin_amdgcn_exp2f((s_m[k][col] * to2 - kRise<T>) - ref), l);
         bad |= s_flag[k];
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -828,14 +852,14 @@ __global__ __launch_bounds__(NTJ) void k_attn_join(AttnArgs p) {
         const int i = f % 4, at = 32 * (d0 + f / 4) + 8 * i + 4 * half;
         float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int k = 0; k < parts; ++k) {
-            const float g = __builtin_amdgcn_exp2f(s_m[k][col] * to2 - ref);
+            const float g = __builtin_amdgcn_exp2f((s_m[k][col] * to2 - kRise<T>) - ref);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = __fmaf_rn(s_o[k][f / 4][4 * i + e][lane], g, x[e]);
         }
         if (r >= rows || at >= c.D) continue;
         *(uint2*)(out + at) =
             make_uint2(pack2<T>(x[0] * inv, x[1] * inv), pack2<T>(x[2] * inv, x[3] * inv));
-        if (a.lse && at == 0) a.lse[qrow * c.H + qh] = m * a.scale + logf(l);
+        if (a.lse && at == 0) a.lse[qrow * c.H + qh] = lse_of<T>(m, l, a.scale);
         if (bad) add_unfinite<T>(p, b, hk, sq, qi, out, at, c.D);
     }
 }
