@@ -282,10 +282,10 @@ int32_t rheo_node_count(const rheo_tree* tree);
  * table[b][e / page_size] * page_size + e % page_size.  lens[b] entries are
  * the prefix; the rows of one step (the pruned tree, root first, or any
  * other rows) are the entries lens[b] + i behind it.  One step is
- *     rheo_cache_plan        pages and slots for the rows of the step
- *     per layer: rheo_cache_write, rheo_tree_attention
+ *     rheo_cache_plan        pages and slots for the rows of the step; its status
+ *     per layer: rheo_cache_write, rheo_tree_attention (of the served)
  *     (rheo_verify)
- *     rheo_cache_commit      the accepted path moved together, lens advanced
+ *     rheo_cache_commit_served   the accepted path moved together, lens advanced
  *     rheo_token_logprobs    (of what was emitted, where asked for)
  * The caller owns the pages, tables and lengths; the handle owns workspace
  * and an error flag.  The conventions above hold: device pointers,
@@ -298,6 +298,14 @@ int32_t rheo_node_count(const rheo_tree* tree);
  * value out of range sets a bit of the error flag (rheo_cache_error) and
  * never reads or writes outside the arrays as declared by the arguments.
  * n = 0 rows: rheo_cache_write and rheo_tree_attention do nothing.
+ * A sequence that rheo_cache_plan could not serve (status not 0) has no place for
+ * its rows: its row of the table still names pages behind those that it holds, and
+ * they may be another sequence's by now.  rheo_cache_write leaves it out by its
+ * slots of -1; rheo_tree_attention (`status` of its arguments) and the commit
+ * (rheo_cache_commit_served) have to be given the plan's status, or a count of
+ * 0 and an accept_len below 0, and rheo_token_logprobs the commit's path.  Then
+ * nothing of it changes in the step, and its rows of q_out and out are left as they
+ * were (of a new buffer: anything; rheo_verify wants logits that are no NaN).
  * ------------------------------------------------------------------------ */
 
 typedef struct rheo_cache rheo_cache;
@@ -409,6 +417,8 @@ typedef struct rheo_attention_args {
     void* out;                   /* as q; overlaps neither q nor the pages               */
     float* lse;                  /* [B * n][heads] or NULL: log of the sum of
                                     exp(scale q.k) over what the row attends            */
+    const int32_t* status;       /* [B] as rheo_cache_plan wrote it, or NULL: a sequence of
+                                    status not 0 is left out, as with a count of 0      */
 } rheo_attention_args;
 
 /* Attention of the step's rows over the pages: softmax(scale q.k) v over the
@@ -434,6 +444,14 @@ int rheo_cache_commit(rheo_cache* cache, int32_t n, int32_t depth, const int32_t
                       const int32_t* token, const int32_t* accepted, const int32_t* accept_len,
                       const int32_t* lens, const int32_t* table, void* k_cache, void* v_cache,
                       int32_t* path, int32_t* new_lens, void* stream);
+/* The same for the sequences that rheo_cache_plan served: one of status [B] not 0
+ * is treated as one of accept_len < 0, whatever its accept_len.  status NULL: as
+ * rheo_cache_commit. */
+int rheo_cache_commit_served(rheo_cache* cache, int32_t n, int32_t depth, const int32_t* parent,
+                             const int32_t* token, const int32_t* accepted,
+                             const int32_t* accept_len, const int32_t* lens, const int32_t* table,
+                             const int32_t* status, void* k_cache, void* v_cache, int32_t* path,
+                             int32_t* new_lens, void* stream);
 
 /* ---------------------------------------------------------------------------
  * Log probabilities of given tokens

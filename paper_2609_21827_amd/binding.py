@@ -28,6 +28,7 @@ EXPORTS = ["rheo_create", "rheo_create_static", "rheo_destroy", "rheo_begin_step
            "rheo_read_nodes", "rheo_device_error", "rheo_node_count",
            "rheo_cache_create", "rheo_cache_destroy", "rheo_cache_error", "rheo_cache_plan",
            "rheo_cache_write", "rheo_tree_attention", "rheo_cache_commit",
+           "rheo_cache_commit_served",
            "rheo_scorer_create", "rheo_scorer_destroy", "rheo_token_logprobs",
            "rheo_last_error"]
 
@@ -63,7 +64,7 @@ class AttentionArgs(ctypes.Structure):
     _fields_ = [("n", _I32), ("tail", _I32), ("q", _VP), ("q_stride", _I64),
                 ("out_stride", _I64), ("k_cache", _VP), ("v_cache", _VP), ("table", _VP),
                 ("lens", _VP), ("count", _VP), ("mask", _VP), ("scale", _F32), ("out", _VP),
-                ("lse", _VP)]
+                ("lse", _VP), ("status", _VP)]
 
 
 class RheoError(RuntimeError):
@@ -107,6 +108,7 @@ def load_library(path=LIB_PATH):
         "rheo_cache_write": ([vp, ctypes.POINTER(WriteArgs), vp], ctypes.c_int),
         "rheo_tree_attention": ([vp, ctypes.POINTER(AttentionArgs), vp], ctypes.c_int),
         "rheo_cache_commit": ([vp, i32, i32] + [vp] * 11, ctypes.c_int),
+        "rheo_cache_commit_served": ([vp, i32, i32] + [vp] * 12, ctypes.c_int),
         "rheo_scorer_create": ([i32, i32, ctypes.c_int64, ctypes.POINTER(vp)], ctypes.c_int),
         "rheo_scorer_destroy": ([vp], ctypes.c_int),
         "rheo_token_logprobs": ([vp, vp, i32, i32, vp, vp, i32, i32, f32] + [vp] * 6, ctypes.c_int),
@@ -426,7 +428,8 @@ class Cache(_OnDevice):
              stream=None):
         """Pages and slots for the next n rows of each sequence; (slots [B, n] int64,
         positions [B, n] int32, status [B] int32).  held, table, free_list and
-        free_count are updated in place."""
+        free_count are updated in place.  A sequence of status not 0 has no place for its
+        rows; attention and commit are given the status, or they meet pages of others."""
         B, i32 = self.B, self._i32
         one, rows = (B,), (B, n)
         slots, positions, status = out or (None, None, None)
@@ -481,11 +484,12 @@ class Cache(_OnDevice):
         return out
 
     def attention(self, q, k_cache, v_cache, table, lens, mask=None, tail=None, count=None,
-                  scale=None, out=None, lse=None, stream=None):
+                  scale=None, out=None, lse=None, status=None, stream=None):
         """Attention of q [B, n, heads, head_dim] over each sequence's prefix (lens) and the
         ``tail`` entries behind it (by default the mask's columns, or n) that mask [B, n,
         tail] uint8 names; without a mask, causal.  Returns out, or (out, lse) where lse is
-        True or a tensor [B, n, heads] float32.  scale: 1 / sqrt(head_dim) by default."""
+        True or a tensor [B, n, heads] float32.  scale: 1 / sqrt(head_dim) by default.
+        status: the plan's; sequences that it did not serve are left out."""
         B, n = self.B, q.shape[1]
         p_q, q_row = self._rows(q, n, self.H, "q")
         if tail is None:
@@ -505,29 +509,31 @@ class Cache(_OnDevice):
             n, tail, p_q, q_row, out_row, self._pages(k_cache, "k_cache"),
             self._pages(v_cache, "v_cache"), p_table, self._i32(lens, (B,), "lens"),
             self._i32(count, (B,), "count"), p_mask,
-            float(self.D ** -0.5 if scale is None else scale), p_out, p_lse)
+            float(self.D ** -0.5 if scale is None else scale), p_out, p_lse,
+            self._i32(status, (B,), "status"))
         _check(_LIB.rheo_tree_attention(
             self._h, ctypes.byref(a),
             self._stream(stream, (q, k_cache, v_cache, table, lens, count, mask, out,
-                                  lse if both else None))))
+                                  lse if both else None, status))))
         return (out, lse) if both else out
 
     def commit(self, parent, token, accepted, accept_len, lens, table, k_cache, v_cache,
-               out=None, stream=None):
+               out=None, status=None, stream=None):
         """Moves the entries of the accepted path together in all layers; (path [B, depth +
-        1] int32, new lens [B] int32).  ``out``'s second tensor may be lens itself."""
+        1] int32, new lens [B] int32).  ``out``'s second tensor may be lens itself.
+        status: the plan's; sequences that it did not serve keep entries and length."""
         B, n, depth, i32 = self.B, parent.shape[-1], accepted.shape[-1], self._i32
         one, rows = (B,), (B, n)
         path, new_lens = out or (None, None)
         path, p_path = self._made(path, torch.int32, (B, depth + 1), "path", stream)
         new_lens, p_new = self._made(new_lens, torch.int32, one, "new_lens", stream)
-        _check(_LIB.rheo_cache_commit(
+        _check(_LIB.rheo_cache_commit_served(
             self._h, n, depth, i32(parent, rows, "parent"), i32(token, rows, "token"),
             i32(accepted, (B, depth), "accepted"), i32(accept_len, one, "accept_len"),
-            i32(lens, one, "lens"), i32(table, (B, self.width), "table"),
+            i32(lens, one, "lens"), i32(table, (B, self.width), "table"), i32(status, one, "status"),
             self._pages(k_cache, "k_cache", self.layers),
             self._pages(v_cache, "v_cache", self.layers), p_path, p_new,
-            self._stream(stream, (parent, token, accepted, accept_len, lens, table, k_cache,
+            self._stream(stream, (parent, token, accepted, accept_len, lens, table, status, k_cache,
                                   v_cache, path, new_lens))))
         return path, new_lens
 

@@ -90,7 +90,8 @@ __device__ __forceinline__ Seq seq_of(const AttnArgs& p, int b) {
     Seq s;
     const int64_t room = (int64_t)p.c.width << p.c.page_shift;
     s.len = p.a.lens[b];
-    const int count = p.a.count ? p.a.count[b] : p.a.n;
+    int count = p.a.count ? p.a.count[b] : p.a.n;
+    if (p.a.status && p.a.status[b]) count = 0;      // not served: no row of it is there
     s.rows = min(max(count, 0), p.a.n);
     if (count != s.rows) atomicOr(p.c.err, CE_PLAN);
     s.tail = max(p.a.tail - (p.a.n - s.rows), 0);

@@ -229,6 +229,7 @@ int rheo_tree_attention(rheo_cache* c, const rheo_attention_args* args, void* st
     if ((rc = check_words(a.table, 4, "table")) || (rc = check_words(a.lens, 4, "lens"))) return rc;
     if (a.count && (rc = check_words(a.count, 4, "count"))) return rc;
     if (a.lse && (rc = check_words(a.lse, 4, "lse"))) return rc;
+    if (a.status && (rc = check_words(a.status, 4, "status"))) return rc;
     OnDevice on(c->device);
     if (on.error() != hipSuccess) return hip_fail(on.error(), "hipSetDevice");
     return launched(launch_tree_attention(d, a, (hipStream_t)stream), "tree attention launch");
@@ -238,6 +239,15 @@ int rheo_cache_commit(rheo_cache* c, int32_t n, int32_t depth, const int32_t* pa
                       const int32_t* token, const int32_t* accepted, const int32_t* accept_len,
                       const int32_t* lens, const int32_t* table, void* k_cache, void* v_cache,
                       int32_t* path, int32_t* new_lens, void* stream) {
+    return rheo_cache_commit_served(c, n, depth, parent, token, accepted, accept_len, lens, table,
+                                    nullptr, k_cache, v_cache, path, new_lens, stream);
+}
+
+int rheo_cache_commit_served(rheo_cache* c, int32_t n, int32_t depth, const int32_t* parent,
+                             const int32_t* token, const int32_t* accepted,
+                             const int32_t* accept_len, const int32_t* lens, const int32_t* table,
+                             const int32_t* status, void* k_cache, void* v_cache, int32_t* path,
+                             int32_t* new_lens, void* stream) {
     if (!c) return fail(RHEO_EINVAL, "NULL cache");
     const CacheDev& d = c->dev;
     int rc = check_rows(d, n, 1);
@@ -250,11 +260,12 @@ int rheo_cache_commit(rheo_cache* c, int32_t n, int32_t depth, const int32_t* pa
         (rc = check_ptr(v_cache, "v_cache")) || (rc = check_words(path, 4, "path")) ||
         (rc = check_words(new_lens, 4, "new_lens")))
         return rc;
+    if (status && (rc = check_words(status, 4, "status"))) return rc;
     if (new_lens != lens && overlap(new_lens, 4 * (size_t)d.B, lens, 4 * (size_t)d.B))
         return fail(RHEO_EINVAL, "new_lens overlaps lens");
     OnDevice on(c->device);
     if (on.error() != hipSuccess) return hip_fail(on.error(), "hipSetDevice");
-    const CommitArgs a{n, depth, parent, token, accepted, accept_len, lens, table,
+    const CommitArgs a{n, depth, parent, token, accepted, accept_len, lens, table, status,
                        (char*)k_cache, (char*)v_cache, path, new_lens};
     return launched(launch_cache_commit(d, a, (hipStream_t)stream), "cache commit launch");
 }

@@ -27,7 +27,7 @@ __global__ __launch_bounds__(NTC) void k_cache_commit(CacheDev c, CommitArgs a, 
     const int b = blockIdx.x / split, part = blockIdx.x - b * split;
     const int tid = threadIdx.x, lane = tid & 63;
     if (tid < 64) {
-        const int len = a.lens[b], took = a.accept_len[b];
+        const int len = a.lens[b], took = a.status && a.status[b] ? -1 : a.accept_len[b];
         const int32_t* parent = a.parent + (int64_t)b * a.n;
         const int32_t* token = a.token + (int64_t)b * a.n;
         int bad = 0;

@@ -34,6 +34,7 @@ struct PlanArgs {
 struct CommitArgs {
     int n, depth;
     const int32_t *parent, *token, *accepted, *accept_len, *lens, *table;
+    const int32_t* status;         // or NULL
     char *k_cache, *v_cache;
     int32_t *path, *new_lens;
 };

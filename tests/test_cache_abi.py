@@ -82,3 +82,11 @@ def test_pools_past_64_bits_are_refused(bad):
     test_invalid_cache_configs_are_refused(bad)
     from paper_2609_21827_amd import binding
     assert "2^48" in binding.load_library().rheo_last_error().decode()
+
+
+@needs_lib
+def test_a_commit_of_the_served_without_a_handle_is_refused():
+    from paper_2609_21827_amd import binding
+    lib = binding.load_library()
+    assert lib.rheo_cache_commit_served(None, 1, 1, *[None] * 12) == binding.RHEO_EINVAL
+    assert lib.rheo_last_error().decode()
