@@ -28,6 +28,17 @@ __device__ __forceinline__ Demand demand_of(const CacheDev& c, const PlanArgs& a
 __device__ __forceinline__ int clamp31(int64_t v) {
     return (int)(v < 0x7FFFFFFF ? v : 0x7FFFFFFF);
 }
+// Lacked pages may add up to 2^42, of which only sums below the pool's 2^31 are told
+// apart: all others are more than there is.
+__device__ __forceinline__ uint32_t clamp32(int64_t v) {
+    return (uint32_t)(v < 0xFFFFFFFFll ? v : 0xFFFFFFFFll);
+}
+// A sequence's need (at most 2^30 pages) and whether it lacks some; kMisfit: out of range
+// or too many.
+constexpr uint32_t kMisfit = 0xFFFFFFFFu;
+__device__ __forceinline__ uint32_t pack_need(const Demand& d) {
+    return d.fits ? (uint32_t)d.need << 1 | (d.take > 0 ? 1u : 0u) : kMisfit;
+}
 
 }  // namespace
 
@@ -43,15 +54,14 @@ __device__ __forceinline__ int clamp31(int64_t v) {
 // round of loads and one exchange, and a block's rows are worked on all at once: 18 us
 // there (10 without rows), 4 us for one sequence.
 __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
-    // [B + 1] pages lacked by all before, [B + 1] returned; [B] pages needed (-1:
-    // out of range or too many)
+    // [B + 1] pages lacked by all before, [B + 1] returned; [B] pages needed (pack_need)
     extern __shared__ int s_sum[];
     __shared__ int64_t s_wave[2][NTP / 64];
     __shared__ int s_last;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, B = c.B;
-    int* const s_take = s_sum;
-    int* const s_give = s_take + B + 1;
-    int* const s_need = s_give + B + 1;
+    uint32_t* const s_take = (uint32_t*)s_sum;
+    int* const s_give = s_sum + B + 1;
+    uint32_t* const s_need = (uint32_t*)s_give + B + 1;
     // consecutive sequences a thread, then the threads' sums
     const int per = (B + NTP - 1) / NTP, b0 = min(tid * per, B), b1 = min(b0 + per, B);
     const int have0 = *a.free_count;
@@ -70,9 +80,9 @@ __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
         for (int k = 0; k < 4; ++k) {
             if (b + k >= b1) break;
             const Demand d = demand_of(c, a, len[k], count[k], held[k]);
-            s_take[b + k] = clamp31(take);   // (relative to the thread's first)
+            s_take[b + k] = clamp32(take);   // (relative to the thread's first)
             s_give[b + k] = clamp31(give);
-            s_need[b + k] = d.fits ? d.need : -1;
+            s_need[b + k] = pack_need(d);
             take += d.take;
             give += d.give;
             bad |= !d.valid;
@@ -92,11 +102,11 @@ __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
         gives += s_wave[1][w];
     }
     for (int b = b0; b < b1; ++b) {
-        s_take[b] = clamp31(tb + s_take[b]);
+        s_take[b] = clamp32(tb + s_take[b]);
         s_give[b] = clamp31(gb + s_give[b]);
     }
     if (tid == 0) {
-        s_take[B] = clamp31(takes);
+        s_take[B] = clamp32(takes);
         s_give[B] = clamp31(gives);
     }
     const int have = min(max(have0, 0), c.pages);
@@ -104,9 +114,14 @@ __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
     const int64_t room = have + gives;
     __syncthreads();
     if (blockIdx.x == 0 && bad) atomicOr(c.err, CE_PLAN);
+    auto fits = [&](int b) { return s_need[b] != kMisfit; };
+    auto lacks = [&](int b) { return fits(b) && (s_need[b] & 1u); };
+    auto need_of = [&](int b) { return fits(b) ? (int)(s_need[b] >> 1) : 0; };
     auto served = [&](int b) {
-        return s_need[b] >= 0 && (s_take[b + 1] == s_take[b] || s_take[b + 1] <= room);
+        return fits(b) && (!lacks(b) || (int64_t)s_take[b + 1] <= room);
     };
+    // of a served sequence
+    auto took_of = [&](int b) { return (int)(s_take[b + 1] - s_take[b]); };
 
     // page number v of the stack after the pushes
     auto stack_page = [&](int64_t v) -> int {
@@ -123,7 +138,7 @@ __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
                 if (s_give[mid] <= r) lo = mid; else hi = mid - 1;
             }
             // (held out of range as a whole: sums that the index does not follow)
-            const int64_t at = (int64_t)max(s_need[lo], 0) + r - s_give[lo];
+            const int64_t at = (int64_t)need_of(lo) + r - s_give[lo];
             page = a.table[(int64_t)lo * c.width + (at < 0 ? 0 : at < c.width ? at : c.width - 1)];
         }
         if ((unsigned)page >= (unsigned)c.pages) {
@@ -137,9 +152,9 @@ __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
     // pages (16 threads each) and their rows all at once
     const int mine = (B - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
     for (int k = tid / 16; k < mine; k += NTP / 16) {
-        const int b = blockIdx.x + k * gridDim.x, took = s_take[b + 1] - s_take[b];
-        if (!served(b) || !took) continue;
-        const int held = s_need[b] - took;
+        const int b = blockIdx.x + k * gridDim.x;
+        if (!served(b) || !lacks(b)) continue;
+        const int took = took_of(b), held = need_of(b) - took;
         for (int p = tid % 16; p < took; p += 16)
             a.table[(int64_t)b * c.width + held + p] = stack_page(room - 1 - s_take[b] - p);
     }
@@ -153,7 +168,7 @@ __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
         int64_t slot = -1;
         int pos = -1;
         if (served(b) && i < count) {
-            const int held = s_need[b] - (s_take[b + 1] - s_take[b]);    // (or more)
+            const int held = need_of(b) - took_of(b);                    // (or more)
             const int e = len + i, p = e >> c.page_shift;
             const int page = p < held ? a.table[(int64_t)b * c.width + p]
                                       : stack_page(room - 1 - s_take[b] - (p - held));
@@ -169,7 +184,7 @@ __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
     }
     for (int k = tid; k < mine; k += NTP) {
         const int b = blockIdx.x + k * gridDim.x;
-        a.status[b] = served(b) ? 0 : s_need[b] >= 0 ? 1 : 2;
+        a.status[b] = served(b) ? 0 : fits(b) ? 1 : 2;
     }
 
     // every read of this block is done (no data passes to the last block, so the
@@ -186,9 +201,9 @@ __global__ __launch_bounds__(NTP) void k_cache_plan(CacheDev c, PlanArgs a) {
     // pages popped: up to the last sequence that got any
     int used = 0;
     for (int b = b0; b < b1; ++b) {
-        if (s_need[b] >= 0 && s_take[b + 1] > s_take[b] && s_take[b + 1] <= room)
-            used = s_take[b + 1];
-        if (served(b)) a.held[b] = s_need[b];
+        if (!served(b)) continue;
+        if (lacks(b)) used = (int)s_take[b + 1];
+        a.held[b] = need_of(b);
     }
     for (int o = 32; o; o >>= 1) used = max(used, __shfl_xor(used, o));
     if (lane == 0) s_wave[0][wave] = used;
