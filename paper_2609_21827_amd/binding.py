@@ -314,8 +314,6 @@ class _OnDevice:
     def _aside(self, stream):
         """Whether a stream is another than torch's current one; it has to be of the
         handle's device, since its outputs are made and its kernels run there."""
-        if stream is None:
-            return False
         if stream.device_index != self._index:
             _refuse(f"stream must be of {self.device}, got one of device {stream.device_index}")
         return stream.cuda_stream != _current_stream(self._index)
@@ -327,7 +325,7 @@ class _OnDevice:
         work on it to do, and a fill is work of its own: both are in order only for
         calls on that very stream.  So the output is made on the call's stream, and
         torch's current stream, where the caller reads it, is noted with it."""
-        if not self._aside(stream):
+        if stream is None or not self._aside(stream):
             return make(shape, dtype=dtype, device=self.device)
         reader = torch.cuda.current_stream(self._index)
         with torch.cuda.stream(stream):
@@ -338,7 +336,8 @@ class _OnDevice:
     def _made(self, t, dtype, shape, name, stream):
         """(tensor, address) of an output, allocated unless given."""
         if t is None:
-            t = self._new(dtype, shape, stream)
+            t = torch.empty(shape, dtype=dtype, device=self.device) if stream is None else \
+                self._new(dtype, shape, stream)
             return t, t.data_ptr()
         return t, self._dense(t, dtype, shape, name)
 
