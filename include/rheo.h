@@ -297,6 +297,7 @@ int32_t rheo_node_count(const rheo_tree* tree);
  * Lengths, tables, slots and tokens are data that the host cannot check: a
  * value out of range sets a bit of the error flag (rheo_cache_error) and
  * never reads or writes outside the arrays as declared by the arguments.
+ * A call takes up to B * n = 2^30 rows, rheo_cache_write up to 2^26 - 4.
  * n = 0 rows: rheo_cache_write and rheo_tree_attention do nothing.
  * A sequence that rheo_cache_plan could not serve (status not 0) has no place for
  * its rows: its row of the table still names pages behind those that it holds, and
@@ -466,7 +467,7 @@ typedef struct rheo_scorer rheo_scorer;
 int rheo_scorer_create(int32_t vocab, int32_t dtype, int64_t row_stride, rheo_scorer** out);
 int rheo_scorer_destroy(rheo_scorer* scorer);
 
-/* For the token of every entry (b, j), p = softmax(row / T):
+/* For the token of every entry (b, j), fewer than 2^24 in all, p = softmax(row / T):
  *   logits       [B][n][row_stride]
  *   path         [B][m] int32: the entry's row of the sequence's n, or NULL: row j
  *                (m <= n)

@@ -23,6 +23,8 @@ struct rheo_scorer {
 namespace {
 
 constexpr int64_t kMaxRows = (int64_t)1 << 30;   // rows of one call
+// entries of one scoring call: a block of 256 threads each, less than 2^32 in all
+constexpr int64_t kMaxEntries = ((int64_t)1 << 24) - 1;
 
 int zeroed(void** p, size_t bytes) {
     hipError_t e = hipMalloc(p, bytes);
@@ -49,9 +51,9 @@ int check_stride(int64_t stride, int64_t least, const char* name) {
     return RHEO_OK;
 }
 
-int check_rows(const CacheDev& d, int32_t n, int least) {
-    if (n < least || (int64_t)d.B * n > kMaxRows)
-        return fail(RHEO_EINVAL, "n must be in [%d, %lld]", least, (long long)(kMaxRows / d.B));
+int check_rows(const CacheDev& d, int32_t n, int least, int64_t most = kMaxRows) {
+    if (n < least || (int64_t)d.B * n > most)
+        return fail(RHEO_EINVAL, "n must be in [%d, %lld]", least, (long long)(most / d.B));
     return RHEO_OK;
 }
 
@@ -174,7 +176,7 @@ int rheo_cache_write(rheo_cache* c, const rheo_write_args* args, void* stream) {
     if (!c || !args) return fail(RHEO_EINVAL, "NULL argument");
     const rheo_write_args& a = *args;
     const CacheDev& d = c->dev;
-    int rc = check_rows(d, a.n, 0);
+    int rc = check_rows(d, a.n, 0, kWriteRows);
     if (rc) return rc;
     if (a.rot_dim < 0 || a.rot_dim > d.D || a.rot_dim % 2)
         return fail(RHEO_EINVAL, "rot_dim must be even and in [0, head_dim]");
@@ -311,8 +313,8 @@ int rheo_token_logprobs(rheo_scorer* s, const void* logits, int32_t B, int32_t n
                         float T, float* logprob, float* entropy, int32_t* rank,
                         int32_t* top_token, float* top_logprob, void* stream) {
     if (!s) return fail(RHEO_EINVAL, "NULL scorer");
-    if (B < 0 || n < 0 || m < 0 || (int64_t)B * n > kMaxRows || (int64_t)B * m > kMaxRows / 64)
-        return fail(RHEO_EINVAL, "B, n and m must be >= 0, B * n <= 2^30 and B * m <= 2^24");
+    if (B < 0 || n < 0 || m < 0 || (int64_t)B * n > kMaxRows || (int64_t)B * m > kMaxEntries)
+        return fail(RHEO_EINVAL, "B, n and m must be >= 0, B * n <= 2^30 and B * m < 2^24");
     if (!path && m > n) return fail(RHEO_EINVAL, "m must be <= n without a path");
     if (top < 0 || top > 32 || top > s->dev.V)
         return fail(RHEO_EINVAL, "top must be in [0, min(32, vocab)]");

@@ -12,6 +12,9 @@ namespace rheo {
 enum CacheError { CE_PLAN = 1, CE_SLOT = 2, CE_POSITION = 4, CE_PAGE = 8, CE_PATH = 16,
                   CE_TABLE = 32 };
 
+// most rows of a rheo_cache_write: a wave each, and a launch has less than 2^32 threads
+constexpr int64_t kWriteRows = ((int64_t)1 << 26) - 4;
+
 struct CacheDev {
     int B, H, K, D;                // sequences, query heads, key/value heads, head size
     int page_shift, pages, width, layers;

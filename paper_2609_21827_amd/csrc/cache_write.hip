@@ -222,7 +222,7 @@ hipError_t launch_cache_write(const CacheDev& c, const rheo_write_args& a, hipSt
     // units and latency counts
     int parts = (rounds + 3) / 4;
     if ((int64_t)rows * parts < 4096) parts = 4096 / rows < rounds ? 4096 / rows : rounds;
-    if ((int64_t)rows * parts > 1 << 30) parts = 1;
+    if (rows * (int64_t)parts > kWriteRows) parts = (int)(kWriteRows / rows);
     const int64_t waves = (int64_t)rows * parts;
     const int blocks = (int)((waves + NTW / 64 - 1) / (NTW / 64));
     if (c.dtype == RHEO_BF16) start_lph<__bf16>(c, a, blocks, rows, parts, lph, s);
