@@ -74,7 +74,6 @@ struct AttnArgs {
     rheo_attention_args a;
     int g;                         // query heads of a key head
     int groups;                    // most stretches (workgroups)
-    int min_tiles;                 // fewest tiles of a stretch
     int whole;                     // whole items may be given out (see deal_items)
     int* desc;                     // [groups][8]: what k_attn_join adds up
 };
@@ -169,8 +168,7 @@ __device__ Stretch find_stretch(const AttnArgs& p, int w) {
     total = uniform64(total);
     Stretch r;
     r.total = total;
-    const int64_t most = (total + p.min_tiles - 1) / p.min_tiles;
-    r.groups = (int)(most < p.groups ? most : p.groups);
+    r.groups = (int)(total < p.groups ? total : p.groups);
     if (w >= r.groups) {
         r.t0 = r.t1 = 0;
         return r;
@@ -917,7 +915,6 @@ template <typename T, typename S>
 hipError_t start(AttnArgs p, hipStream_t s) {
     static_assert(S::LDS <= 156 * 1024, "LDS");
     p.groups = p.c.slots * S::RESIDENT;
-    p.min_tiles = 1;
     // (fewer items than workgroups: the cuts are what fills them)
     p.whole = (int64_t)p.a.n * p.g <= S::ROWS && p.c.B <= kDealt &&
               (int64_t)p.c.B * p.c.K >= p.groups;
