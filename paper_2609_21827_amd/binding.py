@@ -137,6 +137,24 @@ def _stream(stream):
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+def _output(shape, dtype, device, stream, make=torch.empty):
+    """A new output of a call on `stream` (None: torch's current one).
+
+    Memory comes back to the allocator while the stream that it was made on has still
+    work on it to do, and a fill is work of its own: both are in order only for calls
+    on that very stream.  So the output is made on the call's stream, and torch's
+    current stream, where the caller reads it, is noted with it."""
+    if stream is None:
+        return make(shape, dtype=dtype, device=device)
+    reader = torch.cuda.current_stream(device)
+    if stream.cuda_stream == reader.cuda_stream:
+        return make(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = make(shape, dtype=dtype, device=device)
+    t.record_stream(reader)
+    return t
+
+
 def _current_stream(index):
     """The address of torch's current stream on a device."""
     return _RAW_STREAM(index) if _RAW_STREAM else torch.cuda.current_stream(index).cuda_stream
@@ -204,8 +222,8 @@ class Tree:
 
     def frontier(self, out=None, stream=None):
         if out is None:
-            out = (torch.empty((self.B, self.NE), dtype=torch.int32, device=self.device),
-                   torch.empty((self.B, self.NE), dtype=torch.int32, device=self.device))
+            out = tuple(_output((self.B, self.NE), torch.int32, self.device, stream)
+                        for _ in range(2))
         par, tok = out
         _check(_LIB.rheo_frontier(self._h, _ptr(par), _ptr(tok), _stream(stream)))
         return par, tok
@@ -225,8 +243,8 @@ class Tree:
 
     def pruned_view(self, out=None, stream=None):
         if out is None:
-            out = (torch.empty((self.B, self.R + 1), dtype=torch.int32, device=self.device),
-                   torch.empty((self.B, self.R + 1), dtype=torch.int32, device=self.device))
+            out = tuple(_output((self.B, self.R + 1), torch.int32, self.device, stream)
+                        for _ in range(2))
         par, tok = out
         _check(_LIB.rheo_pruned_view(self._h, _ptr(par), _ptr(tok), _stream(stream)))
         return par, tok
@@ -235,17 +253,16 @@ class Tree:
         """(mask [B][R+1][R+1] uint8, depth [B][R+1] int32) of the pruned tree."""
         n = self.R + 1
         if out is None:
-            out = (torch.empty((self.B, n, n), dtype=torch.uint8, device=self.device),
-                   torch.empty((self.B, n), dtype=torch.int32, device=self.device))
+            out = (_output((self.B, n, n), torch.uint8, self.device, stream),
+                   _output((self.B, n), torch.int32, self.device, stream))
         mask, depth = out
         _check(_LIB.rheo_tree_mask(self._h, _ptr(mask), _ptr(depth), _stream(stream)))
         return mask, depth
 
     def verify(self, target_logits, T, rng_key, out=None, stream=None):
         if out is None:
-            out = (torch.empty((self.B, self.D), dtype=torch.int32, device=self.device),
-                   torch.empty((self.B,), dtype=torch.int32, device=self.device),
-                   torch.empty((self.B,), dtype=torch.int32, device=self.device))
+            out = tuple(_output(shape, torch.int32, self.device, stream)
+                        for shape in ((self.B, self.D), (self.B,), (self.B,)))
         acc, alen, fin = out
         _check(_LIB.rheo_verify(self._h, _ptr(target_logits), float(T),
                                 int(rng_key) & (2 ** 64 - 1), _ptr(acc), _ptr(alen),
@@ -255,9 +272,9 @@ class Tree:
     def read_nodes(self, stream=None):
         shape = (self.B, self.N)
         dev = self.device
-        out = {k: torch.empty(shape, dtype=torch.int32, device=dev)
+        out = {k: _output(shape, torch.int32, dev, stream)
                for k in ("token", "parent", "depth", "slot", "kind")}
-        out.update({k: torch.empty(shape, dtype=torch.float64, device=dev)
+        out.update({k: _output(shape, torch.float64, dev, stream)
                     for k in ("proxy", "qtrue", "score")})
         _check(_LIB.rheo_read_nodes(self._h, *[_ptr(out[k]) for k in (
             "token", "parent", "depth", "slot", "kind", "proxy", "qtrue", "score")],
@@ -319,19 +336,10 @@ class _OnDevice:
         return stream.cuda_stream != _current_stream(self._index)
 
     def _new(self, dtype, shape, stream, make=torch.empty):
-        """A new output of a call on `stream`.
-
-        Memory comes back to the allocator while the stream that it was made on has still
-        work on it to do, and a fill is work of its own: both are in order only for
-        calls on that very stream.  So the output is made on the call's stream, and
-        torch's current stream, where the caller reads it, is noted with it."""
-        if stream is None or not self._aside(stream):
-            return make(shape, dtype=dtype, device=self.device)
-        reader = torch.cuda.current_stream(self._index)
-        with torch.cuda.stream(stream):
-            t = make(shape, dtype=dtype, device=self.device)
-        t.record_stream(reader)
-        return t
+        """A new output of a call on `stream`, which is of the handle's device."""
+        if stream is not None:
+            self._aside(stream)
+        return _output(shape, dtype, self.device, stream, make)
 
     def _made(self, t, dtype, shape, name, stream):
         """(tensor, address) of an output, allocated unless given."""

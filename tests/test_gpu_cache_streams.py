@@ -121,3 +121,42 @@ def test_streams_of_other_libraries(binding):
             assert torch.equal(x, y)
     for h in handles:
         h.close()
+
+
+def _tree(binding, levels):
+    tree = binding.Tree(batch=2, vocab=320, pool=4, leads=1, depth=3, support=64, dtype=BF16)
+    g = torch.Generator().manual_seed(0)
+    tree.begin_step()
+    for level in range(levels):
+        rows = tree.NE if level else 1
+        tree.expand_level(torch.randn((2, rows, 320), generator=g).to(BF16).cuda(), 1.0, 5)
+    return tree, torch.randn((2, 9, 320), generator=g).to(BF16).cuda()
+
+
+@pytest.mark.parametrize("name", ["frontier", "read_nodes", "pruned_view", "tree_mask", "verify"])
+def test_outputs_of_a_trees_calls(binding, name):
+    """As the first test above, for the calls of the tree that make their outputs."""
+    levels = 2 if name == "frontier" else 3            # (the last level has none behind it)
+    (a, target), (b, _) = _tree(binding, levels), _tree(binding, levels)
+    side = torch.cuda.Stream()
+
+    def call(tree, stream):
+        if name in ("pruned_view", "tree_mask", "verify"):
+            tree.prune(8, stream=stream)
+        got = tree.verify(target, 1.0, 5, stream=stream) if name == "verify" else \
+            getattr(tree, name)(stream=stream)
+        return list(got.values()) if isinstance(got, dict) else list(got)
+
+    want = [t.clone() for t in call(a, None)]
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    old = [torch.empty_like(t) for t in want for _ in range(40)]
+    _busy()
+    for t in old:
+        t.fill_(1)
+    del old, t
+    got = call(b, side)
+    torch.cuda.synchronize()
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+    a.close(), b.close()
