@@ -73,9 +73,9 @@ struct AttnArgs {
     CacheDev c;
     rheo_attention_args a;
     int g;                         // query heads of a key head
+    int* desc;                     // [groups][8]: what k_attn_join adds up
     int groups;                    // most stretches (workgroups)
     int whole;                     // whole items may be given out (see deal_items)
-    int* desc;                     // [groups][8]: what k_attn_join adds up
 };
 
 // A sequence's part of the line.
