@@ -54,8 +54,8 @@ def test_keys_far_below_a_sink_keep_their_weight(binding, B, n, H, K, D):
     these give is in the output with fp16's own accuracy.
 
     Bound: as the oracle's, but that a probability's rounding where fp16 has no more
-    smaller steps, 2^-25 at most, is against a sum of at least 2^11 (the kernel's
-    reference for fp16) and not of 1."""
+    smaller steps, 2^-25 at most, is against a sum of at least 2^10 (the kernel's
+    reference for fp16: the largest probability is held as 2^10 to 2^15) and not of 1."""
     L, page = 2000, 16
     g = torch.Generator().manual_seed(D + n)
     pages = L // page + -(-n // page) + 1
@@ -85,7 +85,7 @@ def test_keys_far_below_a_sink_keep_their_weight(binding, B, n, H, K, D):
         want, w_lse, tol, tol_lse = ref.attention(q[0, rows, h:h + 1], k, v, seen, D ** -0.5, F16)
         for i in range(len(rows)):
             size = v[seen[i]].double().abs().sum(0)
-            tol[i] += ref.TINY[F16] * (2.0 ** -11 * size + 1) - ref.TINY[F16] * (size + 1)
+            tol[i] += ref.TINY[F16] * (2.0 ** -10 * size + 1) - ref.TINY[F16] * (size + 1)
         assert float((tol / want.abs()).max()) < 0.01
         for b in range(B):
             off = (out[b, rows, h:h + 1].double() - want).abs()
