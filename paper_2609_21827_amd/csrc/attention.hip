@@ -22,13 +22,17 @@
 // adds up.
 //
 // What bounds it: few rows, memory: 128 single tokens over 8191 entries (4 key heads of
-// 128, fp16, 1.34 GB) 263 us, 5.1 TB/s.  Up to 256 rows, the products and the softmax
+// 128, fp16, 1.34 GB) 260 us, 5.2 TB/s.  Up to 256 rows, the products and the softmax
 // beside them: 64 trees of 244 rows over 1000 to 4096 entries (8 key heads, 0.79 GB,
-// 176 GFLOP) 236 us, 745 TFLOP/s.  There the loads alone take 180 us and the rest alone
-// 218; a SIMD's two waves keep its matrix core busy for 178 of 425 thousand cycles and its
-// vector unit for 204 (an exponential is 16 cycles, the other operations 4): the two
-// hardly overlap, whether the waves are kept in step or not, products and exponentials
-// of one wave interleaved (10 to 20 us slower) or one wave given priority (no change).
+// 176 GFLOP) 233 us, 755 TFLOP/s; the floor is 164, by the bytes.  There the loads alone
+// take 180 us and the rest alone 218; a SIMD's two waves keep its matrix core busy for 178
+// of 423 thousand cycles and its vector unit for 202 (an exponential is 16 cycles, the other
+// operations 4), mostly one after the other: both waves pass a barrier at the top of each
+// tile, so they do products together and then exponentials together.  No gain came from
+// waves not kept in step, from products and exponentials of one wave and tile
+// interleaved (10 to 20 us slower) and from one wave given priority.  Scores of the
+// next tile computed beside this one's second product, and the two waves half a tile
+// apart, are not tried.
 #include <type_traits>
 
 #include "cache_state.h"
@@ -199,7 +203,9 @@ __device__ Stretch find_stretch(const AttnArgs& p, int w) {
 // back, as long as some four tiles of 256 rows each, and the join: 64 trees of 244
 // rows over 1000 to 4096 entries 271 us in stretches, 237 dealt.  (Partial results
 // of 64 rows and fewer are too small for that: 3 % slower.)  All threads call it;
-// at most kDealt sequences, an item a key head each.
+// at most kDealt sequences, an item a key head each: every workgroup ranks all sequences
+// by counting, and their order is in LDS.  More are cut (256 sequences of 500 to 2000
+// entries, 61 rows, 32/8 heads, 504 us; 257 560).
 constexpr int kDealt = 256;
 
 __device__ __forceinline__ int dealt_item(int round, int w, int groups) {
@@ -874,12 +880,19 @@ __global__ __launch_bounds__(NTJ) void k_attn_join(AttnArgs p) {
 
 namespace {
 
-// Shapes for up to 32, 64, 128 and more rows of an item: the fastest of those that
-// fit, of two or three tried each.  Few rows are bound by memory, and the waves of
-// a workgroup share the entries; many by the products and the vector work between
-// them.  us for 32 sequences, 8 key heads of 128, 4096 entries (bytes: 64 at the
-// copy's rate) with 4 rows 82 (two waves, three tiles ahead: 86), 40 rows 90 (eight
-// waves: 126; one tile ahead: 115), 100 rows 118 (eight waves: 135), 244 rows 157.
+// Shapes for up to 32, 64, 128 and more rows of an item: for 128 elements the fastest of
+// those that fit, of two or three tried each.  Few rows are bound by memory, and the
+// waves of a workgroup share the entries; many by the products and the vector work
+// between them.  us for 32 sequences of 1024 to 4096 entries, 8 key heads (bytes at the
+// copy's rate: 34, 68, 135 for 64, 128, 256 elements), with
+//                 4 rows   40 rows   100 rows   244 rows
+//   64 elements     49       59        68         114      (the shapes of 128, no others tried)
+//   128             85       90       119         161
+//   256            197      205       208         390
+// Of 128, 4 rows by two waves and three tiles ahead took 1.05 times as long, 40 rows by
+// eight waves 1.4 times and with one tile ahead 1.28, 100 rows by eight waves 1.14.  The
+// kernel for up to 64 rows of 256 elements spills 22 vector registers, most of it
+// between items.
 template <int DT>
 struct Shapes;
 template <>

@@ -360,7 +360,8 @@ template <int DT>
 hipError_t start(const ScoreDev& c, const LogprobArgs& a, hipStream_t s) {
     const int entries = a.B * a.m, chunks = (c.V + CHUNK - 1) / CHUNK;
     // Rows are split while all segments stay below PARTS, eight or nine blocks a
-    // compute unit, into at most 64 (a lane each in the join).  Splitting costs a
+    // compute unit (of which five are resident: 96 registers, 106 for fp32), into at
+    // most 64 (a lane each in the join).  Splitting costs a
     // first chunk's selection a segment and the join: 640 rows of 151936, 20
     // alternatives, 79 us in one to three parts each and 85 in six; but 1152 entries of
     // which half are left out 95 us whole and 80 in halves, since whole they leave
