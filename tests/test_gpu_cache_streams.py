@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from test_gpu_cache import BF16, Setup, _i32, _tree_mask
+from test_gpu_cache_use import Loop
 
 pytestmark = pytest.mark.gpu
 
@@ -159,4 +160,32 @@ def test_outputs_of_a_trees_calls(binding, name):
     torch.cuda.synchronize()
     for x, y in zip(got, want):
         assert torch.equal(x, y)
+    a.close(), b.close()
+
+
+def test_a_step_captured_on_a_forked_stream_replays(binding):
+    """The calls go to a stream that a capture forks to and joins again, with outputs of their
+    own: replays, with eager steps of another loop between them, give what eager steps give."""
+    a, b = Loop(binding), Loop(binding)
+    side, capture = torch.cuda.Stream(), torch.cuda.Stream()
+    a.feed(100), b.feed(100)
+    want = a.step()
+    side.wait_stream(torch.cuda.current_stream())
+    got = b.step(stream=side)
+    torch.cuda.synchronize()
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=capture):
+        side.wait_stream(capture)
+        got = b.step(stream=side)
+        capture.wait_stream(side)
+    for seed in range(4):
+        a.feed(seed), b.feed(seed)
+        want = a.step()
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(got + b.state(), want + a.state()):
+            assert torch.equal(x, y)
+    assert a.cache.device_error() == 0 and b.cache.device_error() == 0
     a.close(), b.close()
