@@ -338,7 +338,8 @@ int rheo_cache_destroy(rheo_cache* cache);
  * rheo_cache_plan, count in rheo_tree_attention; bit 1: a slot >= pages *
  * page_size; bit 2: a position outside the rotation table; bit 3: a page
  * outside the pool; bit 4: an accepted token that is no child, at a higher
- * index, of the node before it; bit 5: entries past the table's row. */
+ * index, of the node before it; bit 5: entries past the table's row; bit 6: an
+ * infinity or NaN rounded to 4 bits (rheo_packed_append, rheo_packed_commit). */
 int rheo_cache_error(rheo_cache* cache, int32_t* host_flag);
 
 /* Pages and slots for the next rows of every sequence.
@@ -453,6 +454,132 @@ int rheo_cache_commit_served(rheo_cache* cache, int32_t n, int32_t depth, const 
                              const int32_t* accept_len, const int32_t* lens, const int32_t* table,
                              const int32_t* status, void* k_cache, void* v_cache, int32_t* path,
                              int32_t* new_lens, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The cache in 4 bits
+ *
+ * Where contexts do not fit the memory in 16 bits, the entries of the prefix are held
+ * in 4, and only the rows of the step at hand are in 16:
+ *   k_pages, v_pages  [layers][pages][kv_heads] heads' pages of bytes,
+ *   k_tail, v_tail    [B][tail] rows of [kv_heads][head_dim] of cfg.dtype, a layer's.
+ * A head's page holds page_size entries (16 or more), of nb = ceil(head_dim / 32)
+ * blocks of 32 elements (elements past head_dim are 0):
+ *   page_size * 16 nb bytes of codes, entry after entry, element 2i of an entry in
+ *       the low half of its byte i, element 2i + 1 in the high half,
+ *   nb * page_size bytes of exponents, block after block, in each entry after entry.
+ * A code's low three bits stand for 0, 0.5, 1, 1.5, 2, 3, 4, 6, its high bit for the
+ * sign; an element is that times 2^(exponent - 127), exactly so in cfg.dtype.  A block's
+ * exponent is e + 127 with, for its largest magnitude m 2^E (1 <= m < 2), e = E - 2 if
+ * m < 1.75, else E - 1, and at least -125 and at most 125 (RHEO_BF16), at least -23
+ * and at most 13 (RHEO_F16); elements are rounded to the nearest code, ties to the even
+ * one, and are 6 at most.
+ * The handle is a rheo_cache whose pages, table and lengths are these (its page_stride
+ * and layer_stride are not used); rheo_cache_plan plans them as any.  One step is
+ *     rheo_cache_plan            pages and slots for what the step may keep
+ *     per layer: rheo_cache_write   into the tail, by a handle whose pages are its rows
+ *                rheo_packed_attention
+ *     (rheo_verify)
+ *     rheo_packed_commit         the accepted path's rows into the pages of all layers
+ * and without a tree rheo_packed_append, a layer at a time, in the commit's place.  The
+ * conventions of the cache hold, on sequences that the plan could not serve also.
+ * ------------------------------------------------------------------------ */
+
+typedef struct rheo_packed_pages {
+    void* k;                     /* [layers][pages][kv_heads] heads' pages              */
+    void* v;
+    int64_t page_stride;         /* bytes between pages, a multiple of 16, at least
+                                    kv_heads heads' pages; 0: equal to it; pages *
+                                    page_stride <= 2^48                               */
+    int64_t layer_stride;        /* bytes between layers, a multiple of 16; 0: pages *
+                                    page_stride                                       */
+} rheo_packed_pages;
+
+/* Bytes of one head's page, page_size * nb * 17. */
+int32_t rheo_packed_page_bytes(int32_t head_dim, int32_t page_size);
+
+typedef struct rheo_packed_rows {
+    int32_t n;                   /* rows of a sequence; row (b, i) is row b * n + i       */
+    int32_t layers;              /* one, or the handle's layers                          */
+    void* k;                     /* [layers][B * n] rows of [kv_heads][head_dim]         */
+    void* v;
+    int64_t row_stride;          /* elements between rows                              */
+    int64_t layer_stride;        /* elements between layers; with one layer not used     */
+    const int64_t* slots;        /* [B * n]; a row of slot < 0 is left out                */
+} rheo_packed_rows;
+
+/* Rows rounded into their slots of the pages.  Slots of one call are distinct (else
+ * what stays in them is undefined).  An infinity is held as the largest code of its
+ * block, a NaN as 0, and neither counts for the block's exponent; both set bit 6 of
+ * the error flag (rheo_cache_error), slots out of range bit 1. */
+int rheo_packed_append(rheo_cache* cache, const rheo_packed_rows* rows,
+                       const rheo_packed_pages* pages, void* stream);
+
+/* The reverse: what the slots hold as rows of cfg.dtype.  Rows without a slot (or with
+ * one out of range) are left as they were. */
+int rheo_packed_read(rheo_cache* cache, const rheo_packed_rows* rows,
+                     const rheo_packed_pages* pages, void* stream);
+
+typedef struct rheo_packed_attention_args {
+    int32_t n;                   /* query rows of a sequence; row (b, i) is row b * n + i */
+    int32_t tail;                /* rows of k_tail and v_tail of a sequence, 0..2^24       */
+    int32_t window;              /* entries that a row reaches back, itself the first of
+                                    them, or 0: all                                   */
+    int32_t sinks;               /* entries from the sequence's start on that a window
+                                    does not hide, >= 0                               */
+    const void* q;               /* [B * n] rows of [heads][head_dim]                   */
+    int64_t q_stride, out_stride, tail_stride;   /* elements between rows               */
+    rheo_packed_pages pages;     /* one layer's (layer_stride is not used)               */
+    const void* k_tail;          /* [B * tail] rows; NULL with tail 0                    */
+    const void* v_tail;
+    const int32_t* table;        /* [B][table_width]                                    */
+    const int32_t* lens;         /* [B] entries in the pages                            */
+    const int32_t* count;        /* [B] or NULL: the first count[b] of the n rows are
+                                    there, and the first tail - (n - count[b]) of the
+                                    tail                                              */
+    const uint8_t* mask;         /* [B][n][tail], row i attends tail row j iff not 0;
+                                    NULL: causal, as below                             */
+    const int32_t* positions;    /* [B][n], with a mask and a window: the rows' positions,
+                                    less than lens[b] counting as that; NULL: lens[b]     */
+    float scale;                 /* 2^-100..2^100                                       */
+    void* out;                   /* as q; overlaps none of the inputs                    */
+    float* lse;                  /* [B * n][heads] or NULL                              */
+    const int32_t* status;       /* [B] or NULL: a sequence of status not 0 is left out   */
+} rheo_packed_attention_args;
+
+/* rheo_tree_attention over the pages (entries 0 to lens[b] - 1) and the tail behind them
+ * (entries lens[b] + j).  Without a mask, row i attends up to entry lens[b] + tail - n +
+ * i, its position (so with tail 0 the rows are the pages' last entries).  With a window
+ * it does not attend entries at or below its position - window, but for the first `sinks`;
+ * a mask says all about the tail, the window being about the pages alone then.  A page
+ * none of whose entries some row attends is not read.  Infinite and NaN values of the
+ * tail act on the rows that attend them alone. */
+int rheo_packed_attention(rheo_cache* cache, const rheo_packed_attention_args* args, void* stream);
+
+typedef struct rheo_packed_commit_args {
+    int32_t n;                   /* nodes of a tree, as rheo_cache_commit                */
+    int32_t depth;               /* 1..15                                              */
+    const int32_t* parent;       /* [B][n]                                              */
+    const int32_t* token;        /* [B][n]                                              */
+    const int32_t* accepted;     /* [B][depth]                                          */
+    const int32_t* accept_len;   /* [B]                                                 */
+    const int32_t* lens;         /* [B]                                                 */
+    const int32_t* table;        /* [B][table_width]                                    */
+    const int32_t* status;       /* [B] or NULL                                         */
+    const void* k;               /* [layers][B * n] rows of [kv_heads][head_dim], all of
+                                    the handle's layers: the tree's, in pruned order     */
+    const void* v;
+    int64_t row_stride;          /* elements between rows                              */
+    int64_t layer_stride;        /* elements between layers                            */
+    rheo_packed_pages pages;
+    int32_t* path;               /* [B][depth + 1] out                                  */
+    int32_t* new_lens;           /* [B] out; may be lens itself                          */
+} rheo_packed_commit_args;
+
+/* Keeps the accepted path of a verified tree: the rows of the root and of the accepted
+ * nodes are rounded into entries lens[b] + 0, 1, 2, ... of every layer's pages; path and
+ * new_lens as by rheo_cache_commit.  A sequence that sets an error bit other than 6 keeps
+ * its entries and length. */
+int rheo_packed_commit(rheo_cache* cache, const rheo_packed_commit_args* args, void* stream);
 
 /* ---------------------------------------------------------------------------
  * Log probabilities of given tokens

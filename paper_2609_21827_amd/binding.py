@@ -28,7 +28,8 @@ EXPORTS = ["rheo_create", "rheo_create_static", "rheo_destroy", "rheo_begin_step
            "rheo_read_nodes", "rheo_device_error", "rheo_node_count",
            "rheo_cache_create", "rheo_cache_destroy", "rheo_cache_error", "rheo_cache_plan",
            "rheo_cache_write", "rheo_tree_attention", "rheo_cache_commit",
-           "rheo_cache_commit_served",
+           "rheo_cache_commit_served", "rheo_packed_page_bytes", "rheo_packed_append",
+           "rheo_packed_read", "rheo_packed_attention", "rheo_packed_commit",
            "rheo_scorer_create", "rheo_scorer_destroy", "rheo_token_logprobs",
            "rheo_last_error"]
 
@@ -65,6 +66,30 @@ class AttentionArgs(ctypes.Structure):
                 ("out_stride", _I64), ("k_cache", _VP), ("v_cache", _VP), ("table", _VP),
                 ("lens", _VP), ("count", _VP), ("mask", _VP), ("scale", _F32), ("out", _VP),
                 ("lse", _VP), ("status", _VP)]
+
+
+class PackedPages(ctypes.Structure):
+    _fields_ = [("k", _VP), ("v", _VP), ("page_stride", _I64), ("layer_stride", _I64)]
+
+
+class PackedRows(ctypes.Structure):
+    _fields_ = [("n", _I32), ("layers", _I32), ("k", _VP), ("v", _VP), ("row_stride", _I64),
+                ("layer_stride", _I64), ("slots", _VP)]
+
+
+class PackedAttentionArgs(ctypes.Structure):
+    _fields_ = [("n", _I32), ("tail", _I32), ("window", _I32), ("sinks", _I32), ("q", _VP),
+                ("q_stride", _I64), ("out_stride", _I64), ("tail_stride", _I64),
+                ("pages", PackedPages), ("k_tail", _VP), ("v_tail", _VP), ("table", _VP),
+                ("lens", _VP), ("count", _VP), ("mask", _VP), ("positions", _VP), ("scale", _F32),
+                ("out", _VP), ("lse", _VP), ("status", _VP)]
+
+
+class PackedCommitArgs(ctypes.Structure):
+    _fields_ = [("n", _I32), ("depth", _I32), ("parent", _VP), ("token", _VP), ("accepted", _VP),
+                ("accept_len", _VP), ("lens", _VP), ("table", _VP), ("status", _VP), ("k", _VP),
+                ("v", _VP), ("row_stride", _I64), ("layer_stride", _I64), ("pages", PackedPages),
+                ("path", _VP), ("new_lens", _VP)]
 
 
 class RheoError(RuntimeError):
@@ -109,6 +134,13 @@ def load_library(path=LIB_PATH):
         "rheo_tree_attention": ([vp, ctypes.POINTER(AttentionArgs), vp], ctypes.c_int),
         "rheo_cache_commit": ([vp, i32, i32] + [vp] * 11, ctypes.c_int),
         "rheo_cache_commit_served": ([vp, i32, i32] + [vp] * 12, ctypes.c_int),
+        "rheo_packed_page_bytes": ([i32, i32], ctypes.c_int32),
+        "rheo_packed_append": ([vp, ctypes.POINTER(PackedRows), ctypes.POINTER(PackedPages), vp],
+                               ctypes.c_int),
+        "rheo_packed_read": ([vp, ctypes.POINTER(PackedRows), ctypes.POINTER(PackedPages), vp],
+                             ctypes.c_int),
+        "rheo_packed_attention": ([vp, ctypes.POINTER(PackedAttentionArgs), vp], ctypes.c_int),
+        "rheo_packed_commit": ([vp, ctypes.POINTER(PackedCommitArgs), vp], ctypes.c_int),
         "rheo_scorer_create": ([i32, i32, ctypes.c_int64, ctypes.POINTER(vp)], ctypes.c_int),
         "rheo_scorer_destroy": ([vp], ctypes.c_int),
         "rheo_token_logprobs": ([vp, vp, i32, i32, vp, vp, i32, i32, f32] + [vp] * 6, ctypes.c_int),
@@ -548,6 +580,171 @@ class Cache(_OnDevice):
         flag = ctypes.c_int32(0)
         _check(_LIB.rheo_cache_error(self._h, ctypes.byref(flag)))
         return flag.value
+
+
+class PackedCache(Cache):
+    """The key/value cache of B sequences in 4 bits (see "The cache in 4 bits" in rheo.h).
+    Tables, lengths and the free list are as Cache's, and so is ``plan``; the caller owns
+
+    k_pages, v_pages  one layer's pages [pages, kv_heads, page_bytes] uint8, or all layers'
+                      [layers, pages, ...], of the same strides, a page's bytes dense
+    k_tail, v_tail    the step's own rows [B, tail, kv_heads, head_dim] of ``dtype``
+
+    Rows go into the tail by a Cache whose pages they are (``write`` of that)."""
+
+    def __init__(self, batch, heads, kv_heads, head_dim, page_size, pages, table_width, layers=1,
+                 dtype=torch.bfloat16, device="cuda"):
+        if page_size < 16:
+            _refuse("page_size must be 16 or more")
+        super().__init__(batch, heads, kv_heads, head_dim, page_size, pages, table_width, layers,
+                         dtype, device=device)
+        self.page_bytes = _LIB.rheo_packed_page_bytes(head_dim, page_size)
+        self._head_shape = (pages, kv_heads, self.page_bytes)
+
+    def write(self, *args, **kw):
+        """Not of 4-bit pages, which take finished rows (``append``)."""
+        _refuse("rows are written into the tail, by a Cache whose pages are the tail's rows")
+
+    def _packed(self, k, v, layers=None):
+        """PackedPages of one layer, or of `layers`."""
+        shape = self._head_shape if layers is None else (layers,) + self._head_shape
+        for t, name in ((k, "k_pages"), (v, "v_pages")):
+            if not isinstance(t, torch.Tensor) or t.dtype is not torch.uint8 or t.shape != shape \
+                    or t.get_device() != self._index:
+                _refuse(f"{name} must be {torch.uint8} {shape} on {self.device}")
+        s = k.stride()
+        if v.stride() != s:
+            _refuse("k_pages and v_pages must have the same strides")
+        page = self.K * self.page_bytes
+        if s[-1] != 1 or (self.K > 1 and s[-2] != self.page_bytes):
+            _refuse("a page's bytes must be dense")
+        row = s[-3] if self.pages > 1 else page
+        layer = s[0] if layers is not None and layers > 1 else self.pages * row
+        if row < page or layer < (self.pages - 1) * row + page:
+            _refuse("pages must not overlap")
+        return PackedPages(k.data_ptr(), v.data_ptr(), row, layer)
+
+    def _layers_rows(self, t, n, layers, name):
+        """(address, elements between rows, between layers) of [layers, B, n, kv_heads,
+        head_dim], or of one layer without that dimension."""
+        if layers is None:
+            return (*self._rows(t, n, self.K, name), 0)
+        if not isinstance(t, torch.Tensor) or t.dim() != 5 or t.shape[0] != layers or not layers:
+            _refuse(f"{name} must be {self.dtype} {(layers, self.B, n, self.K, self.D)} on "
+                    f"{self.device}")
+        at, row = self._rows(t[0], n, self.K, name)
+        least = (self.B * n - 1) * row + self.K * self.D
+        layer = t.stride(0) if layers > 1 else least
+        if n and layer < least:
+            _refuse(f"{name}: layers must not overlap")
+        return at, row, layer
+
+    def _of_layers(self, k_pages):
+        """The layers that pages have: None (no such dimension) or a number."""
+        if not isinstance(k_pages, torch.Tensor) or k_pages.dim() not in (3, 4):
+            _refuse(f"k_pages must be [pages, kv_heads, page_bytes] or [layers, ...] on {self.device}")
+        return None if k_pages.dim() == 3 else k_pages.shape[0]
+
+    def _move(self, call, k, v, slots, k_pages, v_pages, layers, stream):
+        n = slots.shape[-1]
+        p_k, row, layer = self._layers_rows(k, n, layers, "k")
+        p_v, v_row, v_layer = self._layers_rows(v, n, layers, "v")
+        if (v_row, v_layer) != (row, layer):
+            _refuse("k and v must have the same strides")
+        rows = PackedRows(n, 1 if layers is None else layers, p_k, p_v, row, layer,
+                          self._dense(slots, torch.int64, (self.B, n), "slots"))
+        pages = self._packed(k_pages, v_pages, layers)
+        _check(call(self._h, ctypes.byref(rows), ctypes.byref(pages),
+                    self._stream(stream, (k, v, slots, k_pages, v_pages))))
+
+    def append(self, k, v, slots, k_pages, v_pages, stream=None):
+        """Rounds rows k and v [B, n, kv_heads, head_dim] ([layers, B, n, ...] into pages of
+        layers) into their slots [B, n] int64; rows of slot -1 are left out."""
+        self._move(_LIB.rheo_packed_append, k, v, slots, k_pages, v_pages, self._of_layers(k_pages),
+                   stream)
+
+    def read(self, slots, k_pages, v_pages, out=None, stream=None):
+        """(k, v) [B, n, kv_heads, head_dim] that the slots [B, n] hold ([layers, B, n, ...] of
+        pages of layers).  Rows of slot -1 are left as they were (new outputs: zeros)."""
+        layers = self._of_layers(k_pages)
+        if out is None:
+            shape = (self.B, slots.shape[-1], self.K, self.D)
+            shape = shape if layers is None else (layers,) + shape
+            out = tuple(self._new(self.dtype, shape, stream, torch.zeros) for _ in range(2))
+        k, v = out
+        self._move(_LIB.rheo_packed_read, k, v, slots, k_pages, v_pages, layers, stream)
+        return k, v
+
+    def attention(self, q, k_pages, v_pages, table, lens, k_tail=None, v_tail=None, mask=None,
+                  window=0, sinks=0, positions=None, count=None, scale=None, out=None, lse=None,
+                  status=None, stream=None):
+        """Attention of q [B, n, heads, head_dim] over each sequence's pages (``lens`` entries)
+        and the tail behind them that mask [B, n, tail] uint8 names; without a mask, causal,
+        the rows being the last n entries.  window: entries that a row reaches back (0: all),
+        but for the first ``sinks``; with a mask, from ``positions`` [B, n] int32 (the
+        plan's; by default the pages' end).  Returns out, or (out, lse) where lse is True or a
+        tensor [B, n, heads] float32.  scale: 1 / sqrt(head_dim) by default.  status: the
+        plan's; sequences that it did not serve are left out."""
+        B, n = self.B, q.shape[1]
+        p_q, q_row = self._rows(q, n, self.H, "q")
+        if (k_tail is None) != (v_tail is None):
+            _refuse("k_tail and v_tail: both or none")
+        tail = tail_row = 0
+        p_kt = p_vt = None
+        if k_tail is not None:
+            tail = k_tail.shape[1]
+            p_kt, tail_row = self._rows(k_tail, tail, self.K, "k_tail")
+            p_vt, v_row = self._rows(v_tail, tail, self.K, "v_tail")
+            if v_row != tail_row:
+                _refuse("k_tail and v_tail must have the same strides")
+        p_table = self._i32(table, (B, self.width), "table")
+        p_mask = None
+        if mask is not None:         # (one without columns has no address, but names nothing)
+            p_mask = self._dense(mask, torch.uint8, (B, n, tail), "mask") or p_table
+        if out is None:
+            out = self._new(self.dtype, (B, n, self.H, self.D), stream)
+        p_out, out_row = self._rows(out, n, self.H, "out")
+        both, p_lse = lse is not None and lse is not False, None
+        if both:
+            lse, p_lse = self._made(None if lse is True else lse, torch.float32, (B, n, self.H),
+                                    "lse", stream)
+        a = PackedAttentionArgs(
+            n, tail, window, sinks, p_q, q_row, out_row, tail_row, self._packed(k_pages, v_pages),
+            p_kt, p_vt, p_table, self._i32(lens, (B,), "lens"), self._i32(count, (B,), "count"),
+            p_mask, self._i32(positions, (B, n), "positions"),
+            float(self.D ** -0.5 if scale is None else scale), p_out, p_lse,
+            self._i32(status, (B,), "status"))
+        _check(_LIB.rheo_packed_attention(
+            self._h, ctypes.byref(a),
+            self._stream(stream, (q, k_pages, v_pages, table, lens, k_tail, v_tail, mask, positions,
+                                  count, out, lse if both else None, status))))
+        return (out, lse) if both else out
+
+    def commit(self, parent, token, accepted, accept_len, lens, table, k, v, k_pages, v_pages,
+               out=None, status=None, stream=None):
+        """Rounds the accepted path's rows of k and v [layers, B, n, kv_heads, head_dim] into
+        the entries behind each sequence's lens, in all layers' pages; (path [B, depth + 1]
+        int32, new lens [B] int32).  ``out``'s second tensor may be lens itself.  status: the
+        plan's; sequences that it did not serve keep entries and length."""
+        B, n, depth, i32 = self.B, parent.shape[-1], accepted.shape[-1], self._i32
+        one, rows = (B,), (B, n)
+        p_k, row, layer = self._layers_rows(k, n, self.layers, "k")
+        p_v, v_row, v_layer = self._layers_rows(v, n, self.layers, "v")
+        if (v_row, v_layer) != (row, layer):
+            _refuse("k and v must have the same strides")
+        path, new_lens = out or (None, None)
+        path, p_path = self._made(path, torch.int32, (B, depth + 1), "path", stream)
+        new_lens, p_new = self._made(new_lens, torch.int32, one, "new_lens", stream)
+        a = PackedCommitArgs(
+            n, depth, i32(parent, rows, "parent"), i32(token, rows, "token"),
+            i32(accepted, (B, depth), "accepted"), i32(accept_len, one, "accept_len"),
+            i32(lens, one, "lens"), i32(table, (B, self.width), "table"), i32(status, one, "status"),
+            p_k, p_v, row, layer, self._packed(k_pages, v_pages, self.layers), p_path, p_new)
+        _check(_LIB.rheo_packed_commit(
+            self._h, ctypes.byref(a),
+            self._stream(stream, (parent, token, accepted, accept_len, lens, table, status, k, v,
+                                  k_pages, v_pages, path, new_lens))))
+        return path, new_lens
 
 
 class Scorer(_OnDevice):

@@ -17,7 +17,7 @@ LIB = os.path.join(HERE, "librheo.so")
 PROBE_LIB = os.path.join(HERE, "libstreamprobe.so")
 SOURCES = ["api.hip", "expand.hip", "dense.hip", "prune.hip", "verify.hip", "views.hip",
            "cache_api.hip", "cache_plan.hip", "cache_write.hip", "attention.hip",
-           "cache_commit.hip", "logprobs.hip"]
+           "cache_commit.hip", "packed_rows.hip", "packed_attention.hip", "logprobs.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 

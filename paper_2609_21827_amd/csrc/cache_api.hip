@@ -63,6 +63,64 @@ bool overlap(const void* p, size_t np, const void* q, size_t nq) {
 
 int launched(hipError_t e, const char* what) { return e == hipSuccess ? RHEO_OK : hip_fail(e, what); }
 
+// The pages of the 4-bit cache as the kernels take them, `layers` of them.
+int check_packed(const CacheDev& d, const rheo_packed_pages& g, int layers, PackedDev* p) {
+    if (d.page_shift < 4) return fail(RHEO_EINVAL, "4-bit pages hold 16 entries or more");
+    int rc = check_ptr(g.k, "pages.k");
+    if (rc || (rc = check_ptr(g.v, "pages.v"))) return rc;
+    p->k = (uint8_t*)g.k;
+    p->v = (uint8_t*)g.v;
+    p->nb = (d.D + 31) / 32;
+    p->head = rheo_packed_page_bytes(d.D, 1 << d.page_shift);
+    const int64_t page = d.K * p->head;
+    p->page_stride = g.page_stride ? g.page_stride : page;
+    if (p->page_stride < page || p->page_stride % 16)
+        return fail(RHEO_EINVAL, "pages.page_stride must hold a page and be a multiple of 16");
+    if (p->page_stride > ((int64_t)1 << 48) / d.pages)
+        return fail(RHEO_EINVAL, "pages * pages.page_stride must be at most 2^48");
+    const int64_t layer = (d.pages - 1) * p->page_stride + page;
+    p->layer_stride = g.layer_stride ? g.layer_stride : d.pages * p->page_stride;
+    if (layers > 1 && (p->layer_stride < layer || p->layer_stride % 16 ||
+                       p->layer_stride > ((int64_t)1 << 48)))
+        return fail(RHEO_EINVAL, "pages.layer_stride must hold a layer and be a multiple of 16");
+    return RHEO_OK;
+}
+
+// Rows of [kv_heads][head_dim], `layers` times B * n of them.
+int check_packed_rows(const CacheDev& d, int32_t n, int layers, const void* k, const void* v,
+                      int64_t row_stride, int64_t layer_stride) {
+    int rc = check_ptr(k, "k");
+    if (rc || (rc = check_ptr(v, "v"))) return rc;
+    if ((rc = check_stride(row_stride, (int64_t)d.K * d.D, "row_stride"))) return rc;
+    const int64_t layer = ((int64_t)d.B * n - 1) * row_stride + (int64_t)d.K * d.D;
+    if (layers > 1 && (layer_stride < layer || layer_stride % 8 ||
+                       layer_stride > ((int64_t)1 << 48)))
+        return fail(RHEO_EINVAL, "layer_stride must hold a layer's rows and be a multiple of 16 bytes");
+    return RHEO_OK;
+}
+
+int packed_rows(rheo_cache* c, const rheo_packed_rows* rows, const rheo_packed_pages* pages,
+                void* stream, hipError_t (*launch)(const CacheDev&, const PackedDev&,
+                                                   const rheo_packed_rows&, hipStream_t),
+                const char* what) {
+    if (!c || !rows || !pages) return fail(RHEO_EINVAL, "NULL argument");
+    const CacheDev& d = c->dev;
+    const rheo_packed_rows& r = *rows;
+    int rc = check_rows(d, r.n, 0);
+    if (rc) return rc;
+    if (r.layers < 1 || r.layers > d.layers)
+        return fail(RHEO_EINVAL, "layers must be in [1, %d]", d.layers);
+    if (r.n == 0) return RHEO_OK;            // (empty arrays may have no address)
+    PackedDev p;
+    if ((rc = check_packed(d, *pages, r.layers, &p)) ||
+        (rc = check_packed_rows(d, r.n, r.layers, r.k, r.v, r.row_stride, r.layer_stride)) ||
+        (rc = check_words(r.slots, 8, "slots")))
+        return rc;
+    OnDevice on(c->device);
+    if (on.error() != hipSuccess) return hip_fail(on.error(), "hipSetDevice");
+    return launched(launch(d, p, r, (hipStream_t)stream), what);
+}
+
 void free_cache(rheo_cache* c) {
     if (c->dev.err) (void)hipFree(c->dev.err);
     if (c->dev.ticket) (void)hipFree(c->dev.ticket);
@@ -118,9 +176,12 @@ int rheo_cache_create(const rheo_cache_config* cfg, rheo_cache** out) {
     int rc = e == hipSuccess ? RHEO_OK : hip_fail(e, "hipGetDevice");
     if (rc == RHEO_OK) rc = zeroed((void**)&d.err, sizeof(int32_t));
     if (rc == RHEO_OK) rc = zeroed((void**)&d.ticket, (d.B + 1) * sizeof(uint32_t));
-    if (rc == RHEO_OK) rc = zeroed((void**)&d.part, attention_workspace(d) * sizeof(float));
+    const size_t one = attention_workspace(d), other = packed_workspace(d);
+    if (rc == RHEO_OK) rc = zeroed((void**)&d.part, (one > other ? one : other) * sizeof(float));
     if (rc == RHEO_OK && (e = prepare_attention(d)) != hipSuccess)
         rc = hip_fail(e, "tree attention set-up");
+    if (rc == RHEO_OK && (e = prepare_packed(d)) != hipSuccess)
+        rc = hip_fail(e, "packed attention set-up");
     if (rc == RHEO_OK && (e = hipDeviceSynchronize()) != hipSuccess)
         rc = hip_fail(e, "initialising a workspace");
     if (rc != RHEO_OK) {
@@ -270,6 +331,76 @@ int rheo_cache_commit_served(rheo_cache* c, int32_t n, int32_t depth, const int3
     const CommitArgs a{n, depth, parent, token, accepted, accept_len, lens, table, status,
                        (char*)k_cache, (char*)v_cache, path, new_lens};
     return launched(launch_cache_commit(d, a, (hipStream_t)stream), "cache commit launch");
+}
+
+int32_t rheo_packed_page_bytes(int32_t head_dim, int32_t page_size) {
+    return page_size * ((head_dim + 31) / 32) * 17;
+}
+
+int rheo_packed_append(rheo_cache* c, const rheo_packed_rows* rows, const rheo_packed_pages* pages,
+                       void* stream) {
+    return packed_rows(c, rows, pages, stream, launch_packed_append, "packed append launch");
+}
+
+int rheo_packed_read(rheo_cache* c, const rheo_packed_rows* rows, const rheo_packed_pages* pages,
+                     void* stream) {
+    return packed_rows(c, rows, pages, stream, launch_packed_read, "packed read launch");
+}
+
+int rheo_packed_attention(rheo_cache* c, const rheo_packed_attention_args* args, void* stream) {
+    if (!c || !args) return fail(RHEO_EINVAL, "NULL argument");
+    const rheo_packed_attention_args& a = *args;
+    const CacheDev& d = c->dev;
+    int rc = check_rows(d, a.n, 0);
+    if (rc) return rc;
+    if ((int64_t)a.n * d.H > kMaxRows) return fail(RHEO_EINVAL, "n * heads must be <= 2^30");
+    if (a.tail < 0 || a.tail > (1 << 24)) return fail(RHEO_EINVAL, "tail must be in [0, 2^24]");
+    if (a.window < 0 || a.sinks < 0) return fail(RHEO_EINVAL, "window and sinks must be >= 0");
+    if (!(a.scale >= 0x1p-100f && a.scale <= 0x1p100f))
+        return fail(RHEO_EINVAL, "scale must be in [2^-100, 2^100]");
+    if (a.n == 0) return RHEO_OK;            // (empty arrays may have no address)
+    PackedDev p;
+    if ((rc = check_packed(d, a.pages, 1, &p))) return rc;
+    if ((rc = check_ptr(a.q, "q")) || (rc = check_ptr(a.out, "out"))) return rc;
+    if ((rc = check_stride(a.q_stride, (int64_t)d.H * d.D, "q_stride"))) return rc;
+    if ((rc = check_stride(a.out_stride, (int64_t)d.H * d.D, "out_stride"))) return rc;
+    if (a.q == a.out) return fail(RHEO_EINVAL, "out must not be q");
+    if (a.tail) {
+        if ((rc = check_ptr(a.k_tail, "k_tail")) || (rc = check_ptr(a.v_tail, "v_tail"))) return rc;
+        if ((rc = check_stride(a.tail_stride, (int64_t)d.K * d.D, "tail_stride"))) return rc;
+    }
+    if ((rc = check_words(a.table, 4, "table")) || (rc = check_words(a.lens, 4, "lens"))) return rc;
+    if (a.count && (rc = check_words(a.count, 4, "count"))) return rc;
+    if (a.positions && (rc = check_words(a.positions, 4, "positions"))) return rc;
+    if (a.lse && (rc = check_words(a.lse, 4, "lse"))) return rc;
+    if (a.status && (rc = check_words(a.status, 4, "status"))) return rc;
+    OnDevice on(c->device);
+    if (on.error() != hipSuccess) return hip_fail(on.error(), "hipSetDevice");
+    return launched(launch_packed_attention(d, p, a, (hipStream_t)stream), "packed attention launch");
+}
+
+int rheo_packed_commit(rheo_cache* c, const rheo_packed_commit_args* args, void* stream) {
+    if (!c || !args) return fail(RHEO_EINVAL, "NULL argument");
+    const rheo_packed_commit_args& a = *args;
+    const CacheDev& d = c->dev;
+    int rc = check_rows(d, a.n, 1);
+    if (rc) return rc;
+    if (a.depth < 1 || a.depth > 15) return fail(RHEO_EINVAL, "depth must be in [1, 15]");
+    PackedDev p;
+    if ((rc = check_packed(d, a.pages, d.layers, &p)) ||
+        (rc = check_packed_rows(d, a.n, d.layers, a.k, a.v, a.row_stride, a.layer_stride)) ||
+        (rc = check_words(a.parent, 4, "parent")) || (rc = check_words(a.token, 4, "token")) ||
+        (rc = check_words(a.accepted, 4, "accepted")) ||
+        (rc = check_words(a.accept_len, 4, "accept_len")) || (rc = check_words(a.lens, 4, "lens")) ||
+        (rc = check_words(a.table, 4, "table")) || (rc = check_words(a.path, 4, "path")) ||
+        (rc = check_words(a.new_lens, 4, "new_lens")))
+        return rc;
+    if (a.status && (rc = check_words(a.status, 4, "status"))) return rc;
+    if (a.new_lens != a.lens && overlap(a.new_lens, 4 * (size_t)d.B, a.lens, 4 * (size_t)d.B))
+        return fail(RHEO_EINVAL, "new_lens overlaps lens");
+    OnDevice on(c->device);
+    if (on.error() != hipSuccess) return hip_fail(on.error(), "hipSetDevice");
+    return launched(launch_packed_commit(d, p, a, (hipStream_t)stream), "packed commit launch");
 }
 
 int rheo_scorer_create(int32_t vocab, int32_t dtype, int64_t row_stride, rheo_scorer** out) {

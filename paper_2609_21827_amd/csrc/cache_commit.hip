@@ -1,12 +1,11 @@
 // The accepted path of a verified tree and its cache entries (rheo_cache_commit).
-#include "cache_state.h"
+#include "commit_walk.h"
 
 namespace rheo {
 
 namespace {
 
 constexpr int NTC = 256;
-constexpr int kDepthMax = 15;                // accepted tokens of a step (rheo_create's limit)
 
 }  // namespace
 
@@ -35,43 +34,9 @@ __global__ __launch_bounds__(NTC) void k_cache_commit(CacheDev c, CommitArgs a, 
         if (took > a.depth || took >= a.n) bad = CE_PATH;
         if (took >= 0 && (len < 0 || (int64_t)len + 1 + took > room)) bad |= CE_TABLE;
         bool good = took >= 0 && !bad;
-        int node = 0;
-        if (lane == 0) s_path[0] = 0;
-        // the first 128 nodes in registers: a level is then no memory's latency
-        int par[2], tok[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int i = min(64 * k + lane, a.n - 1);
-            par[k] = 64 * k + lane < a.n ? parent[i] : -2;
-            tok[k] = token[i];
-        }
         if (good) {
-            const int want_lane = lane < took ? a.accepted[(int64_t)b * a.depth + lane] : -1;
-            for (int j = 0; j < took && good; ++j) {
-                const int want = __shfl(want_lane, j);
-                int found = 0;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint64_t m = __ballot(par[k] == node && tok[k] == want &&
-                                                64 * k + lane > node);
-                    if (m && !found) found = 64 * k + __builtin_ctzll(m);
-                }
-                // (children come behind their parents; only those count, in whatever
-                // tree, so that the path rises as the moves need it)
-                for (int i0 = max(node + 1, 128); i0 < a.n && !found; i0 += 64) {
-                    const int i = i0 + lane;
-                    const bool hit = i < a.n && parent[i] == node && token[i] == want;
-                    const uint64_t m = __ballot(hit);
-                    if (m) found = i0 + __builtin_ctzll(m);
-                }
-                if (!found) {
-                    bad |= CE_PATH;
-                    good = false;
-                } else {
-                    node = found;
-                    if (lane == 0) s_path[j + 1] = node;
-                }
-            }
+            bad |= walk_path(lane, a.n, parent, token, a.accepted + (int64_t)b * a.depth, took, s_path);
+            good = !bad;
         }
         __builtin_amdgcn_wave_barrier();
         // the slots of each entry that moves, packed together in rising order
