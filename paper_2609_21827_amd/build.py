@@ -17,7 +17,9 @@ LIB = os.path.join(HERE, "librheo.so")
 PROBE_LIB = os.path.join(HERE, "libstreamprobe.so")
 SOURCES = ["api.hip", "expand.hip", "dense.hip", "prune.hip", "verify.hip", "views.hip",
            "cache_api.hip", "cache_plan.hip", "cache_write.hip", "attention.hip",
-           "cache_commit.hip", "packed_rows.hip", "packed_attention.hip", "logprobs.hip"]
+           "cache_commit.hip", "packed_rows.hip", "packed_attention.hip",
+           "packed_heads_1_8.hip", "packed_heads_2_7.hip", "packed_heads_3_6.hip",
+           "packed_heads_4_5.hip", "logprobs.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 
@@ -27,8 +29,10 @@ FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 # The default scheduler leaves every LDS read of the attention loop next to the
 # product that takes it; this one keeps the order that the loop asks for
-# (64 trees over 4096 tokens: 242 us against 252; one token over 517: 15.4, 17.3).
-SOURCE_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"]}
+# (64 trees over 4096 tokens: 242 us against 252; one token over 517: 15.4, 17.3; over
+# 4-bit pages 210 against 222).
+ILP = ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"]
+SOURCE_FLAGS = {s: ILP for s in SOURCES if s == "attention.hip" or s.startswith("packed_heads")}
 
 
 def _run(cmd, verbose):

@@ -1,0 +1,1396 @@
+// Attention over 4-bit pages and a 16-bit tail (rheo_packed_attention).
+//
+// o_i = sum_j p_ij v_j with p = softmax_j(scale q_i.k_j), in one pass over the entries
+// with a running maximum and sum, for the g = heads / kv_heads query heads of a key head
+// and a sequence's rows together, as rheo_tree_attention does it.  What differs is where
+// the operands come from: a wave reads codes, 17 bytes for 32 elements, and makes the matrix
+// cores' operands of them in its registers (the values are exact in 16 bits), with nothing
+// passing through LDS and no wave waiting for another before an item's end.
+//
+// Products are transposed, S^T = K Q^T and O^T = V^T P^T, as 16x16x32 tiles; a wave
+// takes 32 entries at a time, two blocks u of 16, and 16 MQ rows.  Lane 16 g + n holds
+//   of K: entry n of each block, elements 8 NB g + 8 s + (0..7) at step s (Q alike), so
+//         that its 4 NB bytes of codes lie together;
+//   of V: elements 2 NB n + (0..2 NB - 1) of the entries 4 g + (0..3) of both blocks;
+//         column n of tile t is element 2 NB n + t, and a tile's operand is the entries'
+//         words of two elements taken apart and joined by pairs of entries;
+//   of S^T: row n, entries 4 g + (0..3) of each block: with the second product's inner
+//         index 8 g + j <-> entry (j < 4 ? 4 g + j of block 0 : 4 g + j - 4 of block 1) its
+//         probabilities are the right operand as they stand;
+//   of O^T: row n, elements 8 NB g + (0..8 NB - 1), next to each other.
+//
+// Work is one line of tiles over all (sequence, key head, block of rows), cut evenly over
+// the workgroups; items that are cut leave partial results, which k_packed_join adds up.
+// With a window an item's tiles are those of the first entries that stay visible and those
+// from the first row's window on.
+#pragma once
+
+#include <type_traits>
+
+#include "packed_format.h"
+#include "softmax_ref.h"
+
+namespace rheo {
+
+namespace {
+
+// A launch's shape: NB blocks of 32 head elements, a workgroup of NW waves, RES of them to a
+// compute unit.  SHARED: the waves have 32 rows each and make a tile's operands together, in
+// LDS (shared_tiles), 64 entries of it.  Else all have the same 16 MQ rows and every
+// fourth 32 entries (own_tiles).
+template <int NB_, bool SHARED_, int MQ_, int NW_, int RES_>
+struct PShape {
+    static constexpr bool SHARED = SHARED_;
+    static constexpr int NB = NB_, MQ = MQ_, NW = NW_, RES = RES_;
+    static constexpr int DP = 32 * NB, NT = 64 * NW;
+    static constexpr int WAVES = (RES * NW + 3) / 4;           // a SIMD
+    static constexpr int RL = SHARED ? 32 : 16;                // rows of a wave's tile: n of a lane,
+    static constexpr int EL = RL * DP / 64;                    // elements of one that a lane holds
+    static constexpr int EC = EL / NB;                         // ... in a chunk of them
+    static constexpr int ROWS = RL * MQ * (SHARED ? NW : 1);   // of an item
+    static constexpr int KT = SHARED ? 64 : 32 * NW;          // entries of a tile
+    static constexpr int ROWB = 2 * DP + 32;                   // see shared_tiles
+    static constexpr int STAGE = KT * (2 * DP + ROWB);
+    // a partial result: O^T as the lanes hold it, maximum and sum of each row, a flag
+    static constexpr int PART = ROWS * DP + 2 * ROWS + 64;
+    static constexpr int RING = NW == 8 ? 3 : 2;             // see shared_tiles
+    static constexpr int LDS = SHARED ? RING * STAGE : (NW - 1) * MQ * EL * 64 * 4;
+    // Element e of a lane's EL, of the lanes' group g (see the mappings above)
+    __device__ __forceinline__ static int element(int g, int e) {
+        return SHARED ? 32 * (e / 16) + 8 * (e % 16 / 4) + 4 * g + e % 4
+                      : 2 * NB * (4 * g + e % 4) + e / 4;
+    }
+};
+
+struct AttnArgs {
+    CacheDev c;
+    PackedDev p;
+    rheo_packed_attention_args a;
+    int g;                         // query heads of a key head
+    int* desc;                     // [groups][8]: what k_packed_join adds up
+    int groups;                    // most stretches (workgroups)
+    int whole;                     // whole items may be given out (see deal_items)
+};
+
+// A sequence's part of the line.
+struct Seq {
+    int len, rows, tail, nrb;      // entries in pages, rows there, tail's, row blocks
+};
+
+template <typename S>
+__device__ __forceinline__ Seq seq_of(const AttnArgs& p, int b) {
+    Seq s;
+    const int64_t room = (int64_t)p.c.width << p.c.page_shift;
+    s.len = p.a.lens[b];
+    int count = p.a.count ? p.a.count[b] : p.a.n;
+    if (p.a.status && p.a.status[b]) count = 0;      // not served: no row of it is there
+    s.rows = min(max(count, 0), p.a.n);
+    if (count != s.rows) atomicOr(p.c.err, CE_PLAN);
+    s.tail = max(p.a.tail - (p.a.n - s.rows), 0);
+    if (s.len < 0 || s.len > room) {
+        if (s.rows) atomicOr(p.c.err, CE_TABLE);
+        s.len = (int)min((int64_t)max(s.len, 0), room);
+    }
+    s.nrb = (s.rows * p.g + S::ROWS - 1) / S::ROWS;
+    return s;
+}
+
+// What a row block attends, as a whole: entries lo to hi, and those before `sinks`; and
+// its tiles.  Tiles of the pages come first, `pages` of them, then the tail's.  Of these
+// the block takes the first `head` and those from `from` on, `count` in all (one at
+// least).
+struct Span {
+    int lo, hi, pages, head, from, count;
+    __device__ __forceinline__ int tile(int k) const { return k < head ? k : k - head + from; }
+};
+
+template <typename S>
+__device__ __forceinline__ Span span_of(const AttnArgs& p, const Seq& s, int rb) {
+    const rheo_packed_attention_args& a = p.a;
+    Span x;
+    x.hi = s.len + s.tail - 1;
+    x.lo = 0;
+    int first = s.len;                               // position of the first row
+    if (!a.mask) {
+        first = s.len + a.tail - a.n + rb * S::ROWS / p.g;
+        const int last = min(((rb + 1) * S::ROWS - 1) / p.g, s.rows - 1);
+        x.hi = min(x.hi, s.len + a.tail - a.n + last);
+    }
+    if (a.window) x.lo = max(first - a.window + 1, 0);
+    x.pages = (s.len + S::KT - 1) / S::KT;
+    const auto tile_of = [&](int e) {
+        return e < s.len ? e / S::KT : x.pages + (e - s.len) / S::KT;
+    };
+    const int end = tile_of(max(x.hi, 0));
+    x.from = x.hi < x.lo ? end : tile_of(x.lo);
+    x.head = a.window && a.sinks && x.hi >= 0 ? min(tile_of(min(a.sinks - 1, x.hi)) + 1, x.from) : 0;
+    x.count = x.head + end - x.from + 1;
+    return x;
+}
+
+// Tiles of all row blocks of a sequence, for one key head.
+template <typename S>
+__device__ __forceinline__ int64_t tiles_of_head(const AttnArgs& p, const Seq& s) {
+    if (p.a.mask) return s.nrb ? (int64_t)s.nrb * span_of<S>(p, s, 0).count : 0;
+    int64_t t = 0;
+    for (int rb = 0; rb < s.nrb; ++rb) t += span_of<S>(p, s, rb).count;
+    return t;
+}
+
+// Addresses in global memory, said so: loads that may be of LDS as well would wait for both.
+template <typename T>
+using Global = const __attribute__((address_space(1))) T*;
+template <typename T>
+__device__ __forceinline__ Global<T> global(const void* q) { return (Global<T>)(const T*)q; }
+// ... that the kernel does not write, of addresses that are the same in all lanes: these go
+// through the scalar cache.
+template <typename T>
+using Constant = const __attribute__((address_space(4))) T*;
+template <typename T>
+__device__ __forceinline__ Constant<T> constant(const void* q) { return (Constant<T>)(uintptr_t)q; }
+template <typename T, int A>
+__device__ __forceinline__ T load(Global<uint8_t> q) {
+    struct __attribute__((packed, aligned(A))) Word { T v; };
+    return ((const __attribute__((address_space(1))) Word*)q)->v;
+}
+
+// What is the same in all lanes, said so: it then takes scalar registers.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform64(int64_t v) {
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+}
+__device__ __forceinline__ Seq uniform(const Seq& s) {
+    return Seq{uniform(s.len), uniform(s.rows), uniform(s.tail), uniform(s.nrb)};
+}
+__device__ __forceinline__ Span uniform(const Span& s) {
+    return Span{uniform(s.lo),   uniform(s.hi),   uniform(s.pages),
+                uniform(s.head), uniform(s.from), uniform(s.count)};
+}
+
+// Stretch w of the line: tiles [t0, t1) of it, the sequence that t0 is in and the tiles
+// before that sequence.  All threads of the block call it.
+struct Stretch {
+    int64_t total, t0, t1, before;
+    int groups, seq;
+};
+
+__device__ __forceinline__ int64_t stretch_start(int64_t total, int groups, int w) {
+    return total * w / groups;
+}
+
+template <typename S>
+__device__ Stretch find_stretch(const AttnArgs& p, int w) {
+    __shared__ int64_t s_wave[S::NW], s_before;
+    __shared__ int s_seq;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, B = p.c.B;
+    const int per = (B + S::NT - 1) / S::NT, b0 = min(tid * per, B), b1 = min(b0 + per, B);
+    int64_t mine = 0;
+    for (int b = b0; b < b1; ++b) mine += p.c.K * tiles_of_head<S>(p, seq_of<S>(p, b));
+    int64_t incl = mine;
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t u = __shfl_up(incl, o);
+        if (lane >= o) incl += u;
+    }
+    if (lane == 63) s_wave[wave] = incl;
+    __syncthreads();
+    int64_t excl = incl - mine, total = 0;
+    for (int v = 0; v < S::NW; ++v) {
+        if (v < wave) excl += s_wave[v];
+        total += s_wave[v];
+    }
+    total = uniform64(total);
+    Stretch r;
+    r.total = total;
+    r.groups = (int)(total < p.groups ? total : p.groups);
+    r.seq = 0;
+    r.before = 0;
+    if (w >= r.groups) {
+        r.t0 = r.t1 = 0;
+        return r;
+    }
+    r.t0 = stretch_start(total, r.groups, w);
+    r.t1 = stretch_start(total, r.groups, w + 1);
+    if (r.t0 >= excl && r.t0 < excl + mine) {
+        int64_t t = excl;
+        for (int b = b0; b < b1; ++b) {
+            const int64_t k = p.c.K * tiles_of_head<S>(p, seq_of<S>(p, b));
+            if (r.t0 < t + k) {
+                s_seq = b;
+                s_before = t;
+                break;
+            }
+            t += k;
+        }
+    }
+    __syncthreads();
+    r.seq = uniform(s_seq);
+    r.before = uniform64(s_before);
+    return r;
+}
+
+// Whole items dealt out instead of stretches, where that is nearly as even: the sequences
+// sorted by length, their items given to the workgroups in order, there and back (the
+// longest with the shortest).  A cut of 256 rows costs their partial results' way out and
+// back.  All threads call it; at most kDealt sequences, an item a key head each.
+constexpr int kDealt = 256;
+
+__device__ __forceinline__ int dealt_item(int round, int w, int groups) {
+    return round * groups + (round & 1 ? groups - 1 - w : w);
+}
+
+template <typename S>
+__device__ bool deal_items(const AttnArgs& p, int64_t total, int* s_order) {
+    __shared__ int s_tiles[kDealt], s_most[S::NW];
+    const int tid = threadIdx.x, B = p.c.B, K = p.c.K, items = B * K;
+    __syncthreads();
+    for (int b = tid; b < B; b += S::NT) {
+        const Seq s = seq_of<S>(p, b);
+        s_tiles[b] = s.nrb ? span_of<S>(p, s, 0).count : 0;
+    }
+    __syncthreads();
+    for (int b = tid; b < B; b += S::NT) {
+        const int mine = s_tiles[b];
+        int rank = 0;
+        for (int o = 0; o < B; ++o) rank += s_tiles[o] > mine || (s_tiles[o] == mine && o < b);
+        s_order[rank] = b;
+    }
+    __syncthreads();
+    int most = 0;
+    for (int w = tid; w < p.groups; w += S::NT) {
+        int sum = 0;
+        for (int r = 0; r * p.groups < items; ++r) {
+            const int i = dealt_item(r, w, p.groups);
+            if (i < items) sum += s_tiles[s_order[i / K]];
+        }
+        most = max(most, sum);
+    }
+    for (int o = 32; o; o >>= 1) most = max(most, __shfl_xor(most, o));
+    if ((tid & 63) == 0) s_most[tid >> 6] = most;
+    __syncthreads();
+    for (int w = 0; w < S::NW; ++w) most = max(most, s_most[w]);
+    const int64_t mean = total / p.groups;
+    return most <= mean + mean / 16 + 8;
+}
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) s16x4* lds_s4;
+
+template <typename T>
+__device__ __forceinline__ f32x16 mfma32(const u32x4& a, const u32x4& b, const f32x16& c) {
+    typedef typename Pack<T>::v8 v8;
+    if constexpr (std::is_same<T, __bf16>::value)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8, a),
+                                                       __builtin_bit_cast(v8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8, a),
+                                                      __builtin_bit_cast(v8, b), c, 0, 0, 0);
+}
+template <typename T>
+__device__ __forceinline__ f32x4 mfma(const u32x4& a, const u32x4& b, const f32x4& c) {
+    typedef typename Pack<T>::v8 v8;
+    if constexpr (std::is_same<T, __bf16>::value)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a),
+                                                       __builtin_bit_cast(v8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a),
+                                                      __builtin_bit_cast(v8, b), c, 0, 0, 0);
+}
+
+// A row's maximum or sum over the four lanes that hold it.
+__device__ __forceinline__ float row_max(float x) {
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float row_sum(float x) {
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
+// Both elements of a word 0 where they are infinite or NaN.
+template <typename T>
+__device__ __forceinline__ uint32_t finite_pair(uint32_t w) {
+    constexpr uint32_t E = Pack<T>::kExp;
+    return ((w & E) == E ? 0 : w & 0xFFFFu) | ((w & E << 16) == E << 16 ? 0 : w & 0xFFFF0000u);
+}
+
+// The blocks of a lane's elements of K at step s, and of its pair p of V.
+template <int NB>
+__device__ __forceinline__ int k_block(int g, int s) { return (NB * g + s) >> 2; }
+template <int NB>
+__device__ __forceinline__ int v_block(int n, int p) { return (NB * n + p) >> 4; }
+
+// What a wave holds of an item: MQ tiles of RL rows, of which lane RL g + n has row n.
+template <typename S>
+struct Rows {
+    typedef std::conditional_t<S::SHARED, f32x16, f32x4> Part;
+    static constexpr int QS = S::SHARED ? 2 * S::NB : S::NB, VL = S::SHARED ? 16 : 4;
+    u32x4 q[S::MQ][QS];
+    Part o[S::MQ][S::EL / VL];
+    float m[S::MQ], l[S::MQ];      // the exponents' reference, a score; the lane's sum
+    int lo[S::MQ], hi[S::MQ];      // entries that the lane's row attends (and sinks)
+    uint32_t mask[S::MQ];          // its row of the mask
+    __device__ __forceinline__ float at(int mq, int e) const { return o[mq][e / VL][e % VL]; }
+};
+
+// The exponents' reference follows a row's own maximum by steps (kSlack), so that O is
+// rescaled once or twice an item.
+template <typename T, typename S>
+__device__ __forceinline__ void follow(Rows<S>& x, const f32x4 (&sc)[S::MQ][2], float to2, float slack) {
+    float mx[S::MQ];
+    bool up = false;
+#pragma unroll
+    for (int mq = 0; mq < S::MQ; ++mq) {
+        mx[mq] = fmaxf(fmaxf(fmaxf(sc[mq][0][0], sc[mq][0][1]), fmaxf(sc[mq][0][2], sc[mq][0][3])),
+                       fmaxf(fmaxf(sc[mq][1][0], sc[mq][1][1]), fmaxf(sc[mq][1][2], sc[mq][1][3])));
+        up |= mx[mq] > x.m[mq] + slack;
+    }
+    if (__any(up)) {
+#pragma unroll
+        for (int mq = 0; mq < S::MQ; ++mq) {
+            const float m = row_max(mx[mq]);
+            const bool mine = m > x.m[mq] + slack;
+            const float f = mine ? __builtin_amdgcn_exp2f((x.m[mq] * to2 - kRise<T>) - ref_of<T>(m, to2))
+                                 : 1.0f;
+            x.l[mq] *= f;
+#pragma unroll
+            for (int t = 0; t < 2 * S::NB; ++t) x.o[mq][t] *= f;
+            x.m[mq] = mine ? m : x.m[mq];
+        }
+    }
+}
+
+// Scores of one row tile to probabilities.  The sum takes them unrounded, the second product
+// in 16 bits, what the matrix cores take.
+template <typename T>
+__device__ __forceinline__ u32x4 weights(const f32x4 (&sc)[2], float m, float to2, float* l) {
+    const float ref = ref_of<T>(m, to2);
+    float e[8], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        e[i] = __builtin_amdgcn_exp2f(__fmaf_rn(sc[i >> 2][i & 3], to2, -ref));
+        sum += e[i];
+    }
+    *l += sum;
+    u32x4 pt;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) pt[i] = pack2<T>(e[2 * i], e[2 * i + 1]);
+    return pt;
+}
+
+// The operands of two tiles of V from the words w of eight entries.
+__device__ __forceinline__ void by_entries(const uint32_t (&w)[8], u32x4* lo, u32x4* hi) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        (*lo)[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x05040100u);
+        (*hi)[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302u);
+    }
+}
+
+// The infinite and NaN values of the tail, which the products left out, added to a lane's
+// elements of chunk c of a finished row that attends them.  Their probabilities are not 0, so
+// the values themselves decide.  Rare and slow.
+template <typename T, typename S>
+__device__ __forceinline__ void add_unfinite(const AttnArgs& p, int b, int hk, const Seq& sq, int qi,
+                                             T* out, int g, int c) {
+    const rheo_packed_attention_args& a = p.a;
+    const int64_t qrow = (int64_t)b * a.n + qi;
+    const int reach = sq.len + a.tail - a.n + qi;
+#pragma unroll 1
+    for (int j = 0; j < sq.tail; ++j) {
+        const int e = sq.len + j;
+        const bool seen = a.mask ? a.mask[qrow * a.tail + j] != 0
+                                 : e <= reach && (!a.window || e > reach - a.window || e < a.sinks);
+        if (!seen) continue;
+        const T* v = (const T*)a.v_tail + ((int64_t)b * a.tail + j) * a.tail_stride + hk * p.c.D;
+#pragma unroll 1
+        for (int i = 0; i < S::EC; ++i) {
+            const int d = S::element(g, c * S::EC + i);
+            if (d >= p.c.D) continue;
+            const float x = (float)v[d];
+            if (!(fabsf(x) < INFINITY)) out[d] = (T)((float)out[d] + x);
+        }
+    }
+}
+
+// A lane's chunk c of a row, f in the order of the lanes' O^T.
+template <typename T, typename S>
+__device__ __forceinline__ void store_chunk(T* out, int g, int c, int D, const float (&f)[S::EC]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (S::SHARED) {
+            const int d = S::element(g, c * 16 + 4 * i);
+            if (d < D)
+                *(uint2*)(out + d) =
+                    make_uint2(pack2<T>(f[4 * i], f[4 * i + 1]), pack2<T>(f[4 * i + 2], f[4 * i + 3]));
+        } else {
+            const int d = S::element(g, c * 8 + i);
+            if (d < D) *(uint32_t*)(out + d) = pack2<T>(f[i], f[4 + i]);
+        }
+    }
+}
+
+// What a wave needs of the item at hand.
+struct Item {
+    int b, hk, rb;
+    Seq sq;
+    Span span;
+    int tile, end_pages, end_tile;           // the stretch's tiles of it: the pages', the tail's
+    int lo_most, hi_least, sinks;            // entries that all rows of the wave attend:
+                                             // lo_most to hi_least
+    // Whether some row attends entry e of the pages; one of the 16 from e on (others are not
+    // read); whether no row attends one of the 32 from e on; whether one of the wave's rows
+    // does not attend one of these.
+    __device__ __forceinline__ bool attended(int e) const {
+        return e < sq.len && e <= span.hi && (e >= span.lo || e < sinks);
+    }
+    __device__ __forceinline__ bool wanted(int e) const {
+        return e < sq.len && e <= span.hi && (e + 15 >= span.lo || e < sinks);
+    }
+    __device__ __forceinline__ bool some_idle(int e) const {
+        return !(e + 31 < sq.len && e + 31 <= span.hi && (e >= span.lo || e + 31 < sinks));
+    }
+    // (of the first `there` entries; those behind the pages are the tail's)
+    __device__ __forceinline__ bool some_hidden(int e, int there) const {
+        return !(e + 31 < there && e + 31 <= hi_least && (e >= lo_most || e + 31 < sinks));
+    }
+    // `attended` of four entries, as bytes
+    __device__ __forceinline__ uint32_t attended_bytes(int e) const {
+        uint32_t keep = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) keep |= attended(e + r) ? 0xFFu << (8 * r) : 0;
+        return keep;
+    }
+};
+
+// A page's first byte, from its number, the same in all lanes.
+__device__ __forceinline__ int64_t page_at(const AttnArgs& p, int page) {
+    page = uniform(page);
+    if ((unsigned)page >= (unsigned)p.c.pages) {
+        if ((threadIdx.x & 63) == 0) atomicOr(p.c.err, CE_PAGE);
+        page = 0;
+    }
+    return page * p.p.page_stride;
+}
+
+// Scores of what a lane's row does not attend made -inf: `entry(i)` is that of score i, behind
+// the pages the tail's row entry(i) - len.
+template <typename S, bool TAIL, int N, typename Entry, typename Score>
+__device__ __forceinline__ void hide(const AttnArgs& p, const Item& it, const Rows<S>& x, int mq, int e0,
+                                     Entry entry, Score score) {
+    const int there = it.sq.len + (TAIL ? it.sq.tail : 0);
+    if (TAIL && p.a.mask) {
+        const Global<uint8_t> row = global<uint8_t>(p.a.mask) + (int64_t)x.mask[mq] * p.a.tail;
+        uint8_t named[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) named[i] = row[min(entry(i), there - 1) - it.sq.len];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            score(i) = (named[i] != 0) & (entry(i) < there) ? score(i) : -INFINITY;
+    } else if (it.some_hidden(e0, there)) {
+        const int hi = min(x.hi[mq], there - 1);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int e = entry(i);
+            score(i) = (e <= hi) & ((e >= x.lo[mq]) | (e < it.sinks)) ? score(i) : -INFINITY;
+        }
+    }
+}
+
+// The exponent of V's pair p among those loaded of a lane's blocks (the first pair's and,
+// unless the lane's pairs all lie in one block, the last one's).
+template <int NB, int SB>
+__device__ __forceinline__ uint32_t v_scale(const uint32_t (&vs)[SB], int n16, int p0, int p) {
+    if constexpr (SB == 1) return vs[0];
+    else return v_block<NB>(n16, p) == v_block<NB>(n16, p0) ? vs[0] : vs[1];
+}
+__device__ __forceinline__ float scale_of_entry(uint32_t w, int j) {
+    return j == 0 ? scale_at<0>(w) : j == 1 ? scale_at<1>(w) : j == 2 ? scale_at<2>(w) : scale_at<3>(w);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t pair_at(uint32_t codes, float f, int byte) {
+    return byte == 0   ? pair_of<T, 0>(codes, f)
+           : byte == 1 ? pair_of<T, 1>(codes, f)
+           : byte == 2 ? pair_of<T, 2>(codes, f)
+                       : pair_of<T, 3>(codes, f);
+}
+
+// An item's tiles by waves that have the same rows and share the entries: codes straight into
+// registers, operands made there, a wave for itself.
+template <typename T, typename S>
+__device__ __forceinline__ void own_tiles(const AttnArgs& p, const Item& it, Rows<S>& x, bool careful) {
+    constexpr int NB = S::NB, MQ = S::MQ;
+    constexpr bool P2 = (NB & (NB - 1)) == 0;
+    constexpr int VW = NB <= 4 ? 1 : 2;              // words of an entry's V a lane
+    constexpr int SB = P2 ? 1 : 2;                   // blocks that these lie in
+    constexpr int KS = P2 ? (NB + 3) / 4 : NB;       // exponents of K a lane
+    const CacheDev& c = p.c;
+    const rheo_packed_attention_args& a = p.a;
+    const int lane = threadIdx.x & 63, n16 = lane & 15, g4 = lane >> 4;
+    const int wt = uniform(threadIdx.x >> 6), D = c.D;
+    const Seq& sq = it.sq;
+    const float to2 = a.scale * kLog2e;              // scores to exponents of 2
+    const float slack = kSlack<T> / to2;
+    const int in_page = (1 << c.page_shift) - 1;
+    const int scales = 16 * NB << c.page_shift;      // where a head's page has its exponents
+    // the lane's offsets from an entry block's first codes and exponents
+    const uint32_t k_at = n16 * 16 * NB + 4 * NB * g4, v_at = 4 * g4 * 16 * NB + NB * n16;
+    uint32_t kx_at[KS], vx_at[SB];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) kx_at[s] = (k_block<NB>(g4, P2 ? 4 * s : s) << c.page_shift) + n16;
+#pragma unroll
+    for (int s = 0; s < SB; ++s)
+        vx_at[s] = (v_block<NB>(n16, s * (NB - 1)) << c.page_shift) + 4 * g4;
+    const Global<int32_t> row_table = global<int32_t>(a.table) + (int64_t)it.b * c.width;
+    const Global<uint8_t> k_head = global<uint8_t>(p.p.k) + it.hk * p.p.head;
+    const Global<uint8_t> v_head = global<uint8_t>(p.p.v) + it.hk * p.p.head;
+
+    // a tile's 32 entries of the wave: their pages, two blocks', and their codes
+    uint32_t rk[2][NB], rks[2][KS], rv[8][VW], rvs[2][SB];
+    int page0 = 0, page1 = 0;
+    const auto begins = [&](int k) { return it.span.tile(k) * S::KT + 32 * wt; };
+    const auto fetch_pages = [&](int k) {
+        if (k >= it.end_pages) return;
+        const int e0 = begins(k);
+        const bool n0 = it.wanted(e0), n1 = it.wanted(e0 + 16);
+        if (!(n0 | n1)) return;
+        page0 = row_table[(n0 ? e0 : e0 + 16) >> c.page_shift];
+        page1 = row_table[(n1 ? e0 + 16 : e0) >> c.page_shift];
+    };
+    const auto fetch = [&](int k) {
+        if (k >= it.end_pages) return;
+        const int e0 = begins(k);
+        if (!(it.wanted(e0) | it.wanted(e0 + 16))) return;
+        const int64_t page[2] = {page_at(p, page0), page_at(p, page1)};
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int i0 = (e0 + 16 * u) & in_page;
+            const Global<uint8_t> kc = k_head + page[u] + i0 * (16 * NB);
+            const Global<uint8_t> vc = v_head + page[u] + i0 * (16 * NB);
+            const Global<uint8_t> kx = k_head + page[u] + scales + i0;
+            const Global<uint8_t> vx = v_head + page[u] + scales + i0;
+#pragma unroll
+            for (int s = 0; s < NB; ++s) rk[u][s] = load<uint32_t, 4>(kc + k_at + 4 * s);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) rks[u][s] = kx[kx_at[s]];
+            // (a lane's NB bytes at any place: the whole words' last may be the next entry's,
+            // or of the exponents behind the last)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < VW; ++i)
+                    rv[4 * u + j][i] = load<uint32_t, VW == NB / 4 ? 4 : 1>(vc + v_at + (j * 16 * NB + 4 * i));
+#pragma unroll
+            for (int s = 0; s < SB; ++s) rvs[u][s] = load<uint32_t, 4>(vx + vx_at[s]);
+        }
+    };
+    // the scores of 32 entries from e0 on
+    const auto hide_all = [&](f32x4 (&sc)[MQ][2], int e0, auto tail) {
+#pragma unroll
+        for (int mq = 0; mq < MQ; ++mq)
+            hide<S, decltype(tail)::value, 8>(
+                p, it, x, mq, e0, [&](int i) { return e0 + 16 * (i >> 2) + 4 * g4 + (i & 3); },
+                [&](int i) -> float& { return ((float*)&sc[mq][0])[i]; });
+    };
+    // scores to O, with V's operands at hand
+    const auto finish = [&](f32x4 (&sc)[MQ][2], const u32x4 (&vo)[2 * S::NB]) {
+        follow<T, S>(x, sc, to2, slack);
+        u32x4 pt[MQ];
+#pragma unroll
+        for (int mq = 0; mq < MQ; ++mq) pt[mq] = weights<T>(sc[mq], x.m[mq], to2, &x.l[mq]);
+#pragma unroll
+        for (int t = 0; t < 2 * S::NB; ++t)
+#pragma unroll
+            for (int mq = 0; mq < MQ; ++mq) x.o[mq][t] = mfma<T>(vo[t], pt[mq], x.o[mq][t]);
+    };
+
+    fetch_pages(it.tile);
+    fetch(it.tile);
+    fetch_pages(it.tile + 1);
+#pragma unroll 1
+    for (int k = it.tile; k < it.end_pages; ++k) {
+        const int e0 = begins(k);
+        if (!(it.wanted(e0) | it.wanted(e0 + 16))) {
+            fetch(k + 1);
+            fetch_pages(k + 2);
+            continue;
+        }
+        if (it.some_idle(e0)) {
+            // what nobody attends is any bytes: its exponents 0, so that its values are finite
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t keep = it.attended_bytes(e0 + 16 * u + 4 * g4);
+#pragma unroll
+                for (int s = 0; s < SB; ++s) rvs[u][s] &= keep;
+            }
+        }
+        f32x4 sc[MQ][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int mq = 0; mq < MQ; ++mq) sc[mq][u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int s = 0; s < NB; ++s) {
+                const float f = scale_of(rks[u][P2 ? s / 4 : s]);
+                const uint32_t w = rk[u][s];
+                const u32x4 ko{pair_of<T, 0>(w, f), pair_of<T, 1>(w, f), pair_of<T, 2>(w, f),
+                               pair_of<T, 3>(w, f)};
+#pragma unroll
+                for (int mq = 0; mq < MQ; ++mq) sc[mq][u] = mfma<T>(ko, x.q[mq][s], sc[mq][u]);
+            }
+        }
+        u32x4 vo[2 * NB];
+#pragma unroll
+        for (int q = 0; q < NB; ++q) {
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                w[j] = pair_at<T>(rv[j][q / 4],
+                                  scale_of_entry(v_scale<NB>(rvs[j >> 2], n16, 0, q), j & 3), q % 4);
+            by_entries(w, &vo[2 * q], &vo[2 * q + 1]);
+        }
+        fetch(k + 1);
+        fetch_pages(k + 2);
+        hide_all(sc, e0, std::false_type());
+        finish(sc, vo);
+    }
+    const Global<uint8_t> kt = global<uint8_t>(a.k_tail) + 2 * it.hk * D;
+    const Global<uint8_t> vt = global<uint8_t>(a.v_tail) + 2 * it.hk * D;
+    const int64_t row_bytes = 2 * a.tail_stride;
+    const int64_t row0 = (int64_t)it.b * a.tail;
+#pragma unroll 1
+    for (int k = max(it.tile, it.end_pages); k < it.end_tile; ++k) {
+        const int j0 = (it.span.tile(k) - it.span.pages) * S::KT + 32 * wt;
+        if (j0 >= sq.tail) continue;
+        f32x4 sc[MQ][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const Global<uint8_t> row = kt + (row0 + min(j0 + 16 * u + n16, sq.tail - 1)) * row_bytes;
+#pragma unroll
+            for (int mq = 0; mq < MQ; ++mq) sc[mq][u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int s = 0; s < NB; ++s) {
+                const int d = 8 * NB * g4 + 8 * s;
+                u32x4 ko = load<u32x4, 16>(row + 2 * min(d, D - 8));
+                if (d >= D) ko = u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int mq = 0; mq < MQ; ++mq) sc[mq][u] = mfma<T>(ko, x.q[mq][s], sc[mq][u]);
+            }
+        }
+        u32x4 vo[2 * NB];
+#pragma unroll
+        for (int q = 0; q < NB; ++q) {
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int at = j0 + 16 * (j >> 2) + 4 * g4 + (j & 3);
+                // (pairs past the head are columns that no one stores)
+                w[j] = load<uint32_t, 4>(vt + (row0 + min(at, sq.tail - 1)) * row_bytes +
+                                         4 * min(NB * n16 + q, D / 2 - 1));
+                if (at >= sq.tail) w[j] = 0;
+                if (careful) w[j] = finite_pair<T>(w[j]);
+            }
+            by_entries(w, &vo[2 * q], &vo[2 * q + 1]);
+        }
+        hide_all(sc, sq.len + j0, std::true_type());
+        finish(sc, vo);
+    }
+}
+
+// An item's tiles by waves of different rows, of the pages or of the tail.  The waves make a
+// tile's operands together and put them into LDS, K as the lanes take it (`lane` of operand
+// i has 16 bytes at (64 i + lane) 16), V as rows of the entries' elements, 32 bytes more than
+// they are apart, so that the reads that transpose 4x16 blocks of them meet no bank twice;
+// then each multiplies them with its own rows, as 32x32x16 tiles (half the instructions of
+// 16x16x32: issuing them is what bounds this loop).  While tile t is worked on, t + 1 is
+// written, whose codes were loaded during t - 1; so a barrier a tile.
+template <typename T, typename S, bool TAIL>
+__device__ __forceinline__ void shared_tiles(const AttnArgs& p, const Item& it, Rows<S>& x,
+                                             bool careful, char* lds) {
+    constexpr int NB = S::NB, KT = S::KT, KS = 2 * NB;
+    // the waves to a chunk of 32 entries, and the blocks of 32 elements that each makes of it
+    constexpr int U = 2, VP = S::NW / U, NS = (NB + VP - 1) / VP;
+    constexpr int V0 = KT * S::DP * 2, ROWB = S::ROWB;       // where a stage has V; bytes between rows
+    const CacheDev& c = p.c;
+    const rheo_packed_attention_args& a = p.a;
+    const int lane = threadIdx.x & 63, n32 = lane & 31, half = lane >> 5;
+    const int wave = uniform(threadIdx.x >> 6), D = c.D;
+    const Seq& sq = it.sq;
+    const float to2 = a.scale * kLog2e;              // scores to exponents of 2
+    const float slack = kSlack<T> / to2;
+    const int in_page = (1 << c.page_shift) - 1;
+    const int vc = wave / VP, part = wave % VP;      // blocks part, part + VP, ... of chunk vc
+    const Global<int32_t> row_table = global<int32_t>(a.table) + (int64_t)it.b * c.width;
+    const Global<uint8_t> k_head = global<uint8_t>(p.p.k) + it.hk * p.p.head;
+    const Global<uint8_t> v_head = global<uint8_t>(p.p.v) + it.hk * p.p.head;
+    const Global<uint8_t> kt = global<uint8_t>(a.k_tail) + 2 * it.hk * D;
+    const Global<uint8_t> vt = global<uint8_t>(a.v_tail) + 2 * it.hk * D;
+    const int64_t row_bytes = 2 * a.tail_stride;
+    const int64_t row0 = (int64_t)it.b * a.tail;
+    const int begin = TAIL ? max(it.tile, it.end_pages) : it.tile;
+    const int end = TAIL ? it.end_tile : it.end_pages;
+    if (begin >= end || (TAIL && sq.tail == 0)) return;
+
+    // Lane 32 h + n makes elements 16 h to 16 h + 15 of its blocks, of entry n of the chunk.
+    // A tile's part as loaded: codes and exponents, or (of the tail) the elements themselves.
+    uint32_t rk[NS][TAIL ? 8 : 2], rv[NS][TAIL ? 8 : 2], rks[NS], rvs[NS];
+    int page = 0;
+    bool outside = false;                            // a page's number is
+    // (the first entry of tile k's chunk: of the pages, or of the tail)
+    const auto first = [&](int k) {
+        const int v = it.span.tile(k);
+        return (TAIL ? v - it.span.pages : v) * KT + 32 * vc;
+    };
+    const auto fetch_pages = [&](int k, bool plain = false) {
+        if (TAIL || (!plain && k >= end)) return;
+        const int e = first(k) + n32;
+        if (plain || it.attended(e)) page = row_table[e >> c.page_shift];
+    };
+    const auto fetch = [&](int k, bool plain = false) {
+        if (!plain && k >= end) return;
+        const int e = first(k);
+        if constexpr (!TAIL) {
+            // (an entry that no row attends is not read: it counts as zeros)
+            const bool in = plain || it.attended(e + n32);
+            if (!in) {
+#pragma unroll
+                for (int s = 0; s < NS; ++s) rk[s][0] = rk[s][1] = rv[s][0] = rv[s][1] = rks[s] = rvs[s] = 0;
+            } else {
+                const bool good = (unsigned)page < (unsigned)c.pages;
+                outside |= !good;
+                const int entry = (e + n32) & in_page;
+                const int64_t at = (int64_t)(good ? page : 0) * p.p.page_stride;
+                const int64_t codes = at + (entry * (16 * NB) + 16 * part + 8 * half);
+                const int64_t exps = at + (((16 * NB + part) << c.page_shift) + entry);
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    // (blocks past the last: the last one's, of no use)
+                    const int up = NB % VP == 0 ? VP * s : min(VP * s, NB - 1 - part);
+                    const u32x2 w = load<u32x2, 8>(k_head + codes + 16 * up);
+                    const u32x2 y = load<u32x2, 8>(v_head + codes + 16 * up);
+                    rk[s][0] = w[0];
+                    rk[s][1] = w[1];
+                    rv[s][0] = y[0];
+                    rv[s][1] = y[1];
+                    rks[s] = k_head[exps + (up << c.page_shift)];
+                    rvs[s] = v_head[exps + (up << c.page_shift)];
+                }
+            }
+        } else {
+            const int64_t row = (row0 + min(e + n32, sq.tail - 1)) * row_bytes;
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    // (elements past the head: the last ones', made 0 in K, of no use in V)
+                    const int d = min(32 * (part + VP * s) + 16 * half + 8 * i, D - 8);
+                    const u32x4 w = load<u32x4, 16>(kt + row + 2 * d), y = load<u32x4, 16>(vt + row + 2 * d);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        rk[s][4 * i + j] = w[j];
+                        rv[s][4 * i + j] = y[j];
+                    }
+                }
+        }
+    };
+    const auto put = [&](int k, int stage, bool plain = false) {
+        if (!plain && k >= end) return;
+        const int e = first(k);
+        char* const ks = lds + stage * S::STAGE + (vc * KS * 64 + n32) * 16;
+        char* const vs = lds + stage * S::STAGE + V0 + (32 * vc + n32) * ROWB + 32 * half;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const int block = part + VP * s;
+            if (NB % VP != 0 && block >= NB) continue;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                u32x4 w, y;
+                if constexpr (!TAIL) {
+                    const float f = scale_of(rks[s]), g = scale_of(rvs[s]);
+                    w = u32x4{pair_of<T, 0>(rk[s][i], f), pair_of<T, 1>(rk[s][i], f),
+                              pair_of<T, 2>(rk[s][i], f), pair_of<T, 3>(rk[s][i], f)};
+                    y = u32x4{pair_of<T, 0>(rv[s][i], g), pair_of<T, 1>(rv[s][i], g),
+                              pair_of<T, 2>(rv[s][i], g), pair_of<T, 3>(rv[s][i], g)};
+                } else {
+                    const bool there = e + n32 < sq.tail, in = 32 * block + 16 * half + 8 * i < D;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        w[j] = in ? rk[s][4 * i + j] : 0;
+                        y[j] = there ? rv[s][4 * i + j] : 0;
+                        if (careful) y[j] = finite_pair<T>(y[j]);
+                    }
+                }
+                *(u32x4*)(ks + ((2 * block + half) * 64 + 32 * i) * 16) = w;
+                *(u32x4*)(vs + 64 * block + 16 * i) = y;
+            }
+        }
+    };
+    const auto barrier = [] {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    };
+    constexpr int ON = S::RING - 1;                  // tiles that are written ahead
+    __syncthreads();                                 // (the stages are free)
+    fetch_pages(begin);
+    fetch(begin);
+    fetch_pages(begin + 1);
+#pragma unroll
+    for (int i = 0; i < ON; ++i) {
+        put(begin + i, i);
+        fetch(begin + i + 1);
+        fetch_pages(begin + i + 2);
+    }
+    barrier();
+    // Tiles k to k + ON + 2 of which all rows attend everything: from `easy` on, before `hard`
+    int easy = end, hard = end;
+    if constexpr (!TAIL) {
+        const int lo = max(it.lo_most, it.span.lo), hi = min(it.hi_least, min(it.span.hi, sq.len - 1));
+        const int shift = it.span.head - it.span.from;
+        easy = max((lo + KT - 1) / KT + shift, it.span.head);
+        hard = min((hi + 1) / KT + shift, end) - ON - 2;
+    }
+    // the lane's place in V's first 4x16 blocks: 4 entries of a half's 16 elements
+    const uint32_t v_at = (4 * half + (lane & 15) / 4) * ROWB +
+                          (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + (lane & 1) * 8;
+    const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    constexpr int AHEAD = KS * U < 6 ? KS * U : 6;
+    const auto k_part = [&](int stage, int i) {      // K's operand i: step i / U of chunk i % U
+        return *(const u32x4*)(lds + stage * S::STAGE + lane * 16 + (i % U * KS + i / U) * 1024);
+    };
+    u32x4 ahead[AHEAD];
+    if constexpr (ON == 2)
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) ahead[i] = k_part(0, i);
+    int stage = 0;                                   // of tile k
+#pragma unroll 1
+    for (int k = begin; k < end; ++k) {
+        const int next = stage + 1 == S::RING ? 0 : stage + 1;
+        const int write = ON == 1 ? next : next + 1 == S::RING ? 0 : next + 1;
+        const bool plain = k >= easy && k < hard;
+        f32x16 sc[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) sc[u] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < KS * U; ++i)
+            sc[i % U] = mfma32<T>(ON == 2 && i < AHEAD ? ahead[i] : k_part(stage, i), x.q[0][i / U], sc[i % U]);
+        // reads ahead of the products
+        __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+        for (int i = 0; i < KS * U - AHEAD; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+        put(k + ON, write, plain);
+        fetch(k + ON + 1, plain);
+        fetch_pages(k + ON + 2, plain);
+        if (!plain) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int e0 = (TAIL ? sq.len : 0) + first(k) + 32 * (u - vc);
+                hide<S, TAIL, 16>(
+                    p, it, x, 0, e0, [&](int i) { return e0 + 4 * half + 8 * (i / 4) + i % 4; },
+                    [&](int i) -> float& { return ((float*)&sc[u])[i]; });
+            }
+        }
+        // The exponents' reference follows the row's own maximum by steps (kSlack), so that
+        // O is rescaled once or twice an item.
+        float mx = sc[0][0];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[u][i]);
+        if (__any(mx > x.m[0] + slack)) {
+            const float m = fmaxf(mx, __shfl_xor(mx, 32));
+            const bool mine = m > x.m[0] + slack;
+            const float f =
+                mine ? __builtin_amdgcn_exp2f((x.m[0] * to2 - kRise<T>) - ref_of<T>(m, to2)) : 1.0f;
+            x.l[0] *= f;
+#pragma unroll
+            for (int d = 0; d < NB; ++d) x.o[0][d] *= f;
+            x.m[0] = mine ? m : x.m[0];
+        }
+        // The sum takes the probabilities unrounded, the second product in 16 bits, what the
+        // matrix cores take.
+        const float ref = ref_of<T>(x.m[0], to2);
+        float sum = 0.0f;
+        const uint32_t vp = lds_at + stage * S::STAGE + V0 + v_at;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                u32x4 pt;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float e0 = __builtin_amdgcn_exp2f(__fmaf_rn(sc[u][8 * j + 2 * i], to2, -ref));
+                    const float e1 = __builtin_amdgcn_exp2f(__fmaf_rn(sc[u][8 * j + 2 * i + 1], to2, -ref));
+                    sum += e0;
+                    sum += e1;
+                    pt[i] = pack2<T>(e0, e1);
+                }
+#pragma unroll
+                for (int d = 0; d < NB; ++d) {
+                    const uint32_t at = vp + (32 * u + 16 * j) * ROWB + 64 * d;
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)at);
+                    const s16x4 hi =
+                        __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)(at + 8 * ROWB));
+                    const s16x8 va = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    x.o[0][d] = mfma32<T>(__builtin_bit_cast(u32x4, va), pt, x.o[0][d]);
+                }
+            }
+        }
+        x.l[0] += sum;
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 1);
+#pragma unroll
+        for (int i = 0; i < NB * U * 2 - 4; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 1);
+        // (past the last tile: what is there, of no use)
+        if constexpr (ON == 2)
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) ahead[i] = k_part(next, i);
+        barrier();
+        stage = next;
+    }
+    if (outside) atomicOr(c.err, CE_PAGE);
+}
+
+}  // namespace
+
+template <typename T, typename S>
+__global__ __launch_bounds__(S::NT) __attribute__((amdgpu_waves_per_eu(S::WAVES, S::WAVES))) void
+k_packed_attention(AttnArgs p) {
+    constexpr int MQ = S::MQ, RL = S::RL;
+    extern __shared__ __align__(16) char s_lds[];
+    __shared__ float s_ml[S::SHARED ? 2 : S::NW * MQ * 16 * 2];
+    __shared__ int s_order[S::SHARED ? kDealt : 1];    // sequences, the longest first
+    const int tid = threadIdx.x, lane = tid & 63, n = lane % RL, g = lane / RL;
+    const int wave = uniform(tid >> 6), tile0 = S::SHARED ? wave : 0;
+    const CacheDev& c = p.c;
+    const rheo_packed_attention_args& a = p.a;
+    const int w = blockIdx.x, D = c.D;
+    const float to2 = a.scale * kLog2e;              // scores to exponents of 2
+
+    Stretch st = find_stretch<S>(p, w);
+    bool dealt = false;
+    if constexpr (S::SHARED)
+        if (p.whole && st.groups == p.groups)
+            dealt = uniform(deal_items<S>(p, st.total, s_order)) != 0;
+    if (tid == 0) p.desc[8 * w] = 0;
+    if (!dealt && st.t0 >= st.t1) return;
+    // the item at hand: sequence, key head, row block, its tile to begin with; the
+    // tiles left of the stretch, or the round of the deal
+    int b = 0, hk = 0, rb = 0, tile = 0, round = 0;
+    int64_t left = 0;
+    Seq sq;
+    auto next_dealt = [&]() {
+        for (; S::SHARED && round * p.groups < c.B * c.K; ++round) {
+            const int i = dealt_item(round, w, p.groups);
+            if (i >= c.B * c.K) continue;
+            b = uniform(s_order[i / c.K]);
+            hk = i % c.K;
+            sq = uniform(seq_of<S>(p, b));
+            if (sq.nrb) {
+                left = uniform(span_of<S>(p, sq, 0).count);
+                ++round;
+                return true;
+            }
+        }
+        return false;
+    };
+    if (dealt) {
+        if (!next_dealt()) return;
+    } else {
+        b = st.seq;
+        sq = uniform(seq_of<S>(p, b));
+        int64_t rel = st.t0 - st.before;
+        const int64_t per_head = tiles_of_head<S>(p, sq);
+        hk = uniform((int)(rel / per_head));
+        rel -= hk * per_head;
+        for (int n; rel >= (n = span_of<S>(p, sq, rb).count); ++rb) rel -= n;
+        rb = uniform(rb);
+        tile = uniform((int)rel);
+        left = st.t1 - st.t0;
+        // the join of the first item, by the first cut inside it
+        const int64_t begins = st.t0 - tile, ends = begins + span_of<S>(p, sq, rb).count;
+        if (tid == 0 && tile > 0 && stretch_start(st.total, st.groups, w - 1) <= begins) {
+            int* d = p.desc + 8 * w;
+            int n = 2;
+            while (stretch_start(st.total, st.groups, w + n - 1) < ends) ++n;
+            d[0] = n;                                // partial results
+            d[1] = 2 * (w - 1) + (stretch_start(st.total, st.groups, w - 1) < begins ? 1 : 0);
+            d[2] = b;
+            d[3] = hk;
+            d[4] = rb;
+        }
+    }
+
+    for (bool first = true; left > 0; first = false) {
+        const Span span = uniform(span_of<S>(p, sq, rb));
+        const int end_tile = (int)min((int64_t)span.count, tile + left);
+        // (of the pages; then the tail's)
+        const int end_pages = min(end_tile, span.from < span.pages ? span.pages - span.from + span.head
+                                                                   : min(span.head, span.pages));
+        Rows<S> x;
+        int lo_most = 0, hi_least = 0x7FFFFFFF;
+#pragma unroll
+        for (int mq = 0; mq < MQ; ++mq) {
+            const int r = rb * S::ROWS + (tile0 + mq) * RL + n;
+            const bool live = r < sq.rows * p.g;
+            const int qi = live ? r / p.g : 0, qh = hk * p.g + (live ? r - qi * p.g : 0);
+            const int64_t qrow = (int64_t)b * a.n + qi;
+            const T* q = (const T*)a.q + qrow * a.q_stride + (int64_t)qh * D;
+#pragma unroll
+            for (int s = 0; s < Rows<S>::QS; ++s) {
+                const int d = S::SHARED ? 16 * s + 8 * g : 8 * S::NB * g + 8 * s;
+                x.q[mq][s] = u32x4{0, 0, 0, 0};
+                if (live && d < D) x.q[mq][s] = *(const u32x4*)(q + d);
+            }
+            int at = sq.len + a.tail - a.n + qi;     // the row's position
+            if (a.mask) at = a.window && a.positions ? max(a.positions[qrow], sq.len) : sq.len;
+            x.hi[mq] = a.mask ? sq.len - 1 : at;
+            x.lo[mq] = a.window ? at - a.window + 1 : 0;
+            x.mask[mq] = (uint32_t)qrow;
+            if (live) {
+                lo_most = max(lo_most, x.lo[mq]);
+                hi_least = min(hi_least, x.hi[mq]);
+            } else {
+                x.hi[mq] = -1;                       // (what it would attend may be any bytes)
+            }
+        }
+        for (int o = 1; o < RL; o <<= 1) {
+            lo_most = max(lo_most, __shfl_xor(lo_most, o));
+            hi_least = min(hi_least, __shfl_xor(hi_least, o));
+        }
+        lo_most = uniform(lo_most);
+        hi_least = uniform(hi_least);
+        const int sinks = a.window ? a.sinks : 0;
+
+        const Item it{uniform(b),         uniform(hk),       uniform(rb), sq,       span, uniform(tile),
+                      uniform(end_pages), uniform(end_tile), lo_most,     hi_least, sinks};
+        bool careful = false;
+        for (;;) {                                   // again where the tail is not finite
+#pragma unroll
+            for (int mq = 0; mq < MQ; ++mq) {
+#pragma unroll
+                for (int t = 0; t < S::EL / Rows<S>::VL; ++t) x.o[mq][t] = 0.0f;
+                x.m[mq] = -INFINITY;
+                x.l[mq] = 0.0f;
+            }
+            if constexpr (S::SHARED) {
+                shared_tiles<T, S, false>(p, it, x, careful, s_lds);
+                shared_tiles<T, S, true>(p, it, x, careful, s_lds);
+            } else {
+                own_tiles<T, S>(p, it, x, careful);
+            }
+            if (careful) break;
+            // A value that is infinite or NaN has left none of its sums finite, a row's that
+            // does not attend it (0 times it is NaN) neither: then once more without them.
+            float z = 0.0f;
+#pragma unroll
+            for (int mq = 0; mq < MQ; ++mq) {
+                float y = 0.0f;
+#pragma unroll
+                for (int e = 0; e < S::EL; ++e) y = __fmaf_rn(x.at(mq, e), 0.0f, y);
+                if (rb * S::ROWS + (tile0 + mq) * RL + n < sq.rows * p.g) z += y;
+            }
+            careful = __syncthreads_or(!(z == 0.0f) && end_tile > end_pages) != 0;
+            if (!careful) break;
+        }
+
+        // a row's lanes put together, and waves of the same rows
+#pragma unroll
+        for (int mq = 0; mq < MQ; ++mq) {
+            if constexpr (S::SHARED) x.l[mq] += __shfl_xor(x.l[mq], 32);
+            else x.l[mq] = row_sum(x.l[mq]);
+        }
+        if constexpr (!S::SHARED) {
+            __syncthreads();                         // (the last item's have been read)
+#pragma unroll
+            for (int mq = 0; mq < MQ; ++mq)
+                if (g == 0) {
+                    s_ml[((wave * MQ + mq) * 16 + n) * 2] = x.m[mq];
+                    s_ml[((wave * MQ + mq) * 16 + n) * 2 + 1] = x.l[mq];
+                }
+            __syncthreads();
+            float* out = (float*)s_lds;
+#pragma unroll
+            for (int mq = 0; mq < MQ; ++mq) {
+                float m = -INFINITY, l = 0.0f;
+#pragma unroll
+                for (int k = 0; k < S::NW; ++k) m = fmaxf(m, s_ml[((k * MQ + mq) * 16 + n) * 2]);
+                const float ref = ref_of<T>(m, to2);
+#pragma unroll
+                for (int k = 0; k < S::NW; ++k) {
+                    const float* ml = s_ml + ((k * MQ + mq) * 16 + n) * 2;
+                    l += ml[1] * __builtin_amdgcn_exp2f((ml[0] * to2 - kRise<T>) - ref);
+                }
+                const float f = __builtin_amdgcn_exp2f((x.m[mq] * to2 - kRise<T>) - ref);
+#pragma unroll
+                for (int t = 0; t < S::EL / 4; ++t) {
+                    x.o[mq][t] *= f;
+                    if (wave > 0)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            out[(((wave - 1) * MQ + mq) * S::EL + 4 * t + r) * 64 + lane] = x.o[mq][t][r];
+                }
+                x.m[mq] = m;
+                x.l[mq] = l;
+            }
+            __syncthreads();
+            if (wave == 0)
+#pragma unroll 1
+                for (int k = 1; k < S::NW; ++k)
+#pragma unroll
+                    for (int mq = 0; mq < MQ; ++mq)
+#pragma unroll
+                        for (int t = 0; t < S::EL / 4; ++t)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                x.o[mq][t][r] += out[(((k - 1) * MQ + mq) * S::EL + 4 * t + r) * 64 + lane];
+        }
+        if (S::SHARED || wave == 0) {
+            const bool whole = tile == 0 && end_tile == span.count;
+            float* part = c.part + (int64_t)(2 * w + (first ? 0 : 1)) * S::PART;
+#pragma unroll
+            for (int mq = 0; mq < MQ; ++mq) {
+                const int rt = tile0 + mq, r = rb * S::ROWS + rt * RL + n;
+                if (whole) {
+                    if (r < sq.rows * p.g) {
+                        const int qi = r / p.g, qh = hk * p.g + r - qi * p.g;
+                        const int64_t qrow = (int64_t)b * a.n + qi;
+                        const float inv = x.l[mq] == 0.0f ? 0.0f : 1.0f / x.l[mq];
+                        T* o = (T*)a.out + qrow * a.out_stride + (int64_t)qh * D;
+#pragma unroll
+                        for (int k = 0; k < S::NB; ++k) {
+                            float f[S::EC];
+#pragma unroll
+                            for (int i = 0; i < S::EC; ++i) f[i] = x.at(mq, k * S::EC + i) * inv;
+                            store_chunk<T, S>(o, g, k, D, f);
+                        }
+                        if (a.lse && g == 0) a.lse[qrow * c.H + qh] = lse_of<T>(x.m[mq], x.l[mq], a.scale);
+                        if (careful)
+                            for (int k = 0; k < S::NB; ++k) add_unfinite<T, S>(p, b, hk, sq, qi, o, g, k);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < S::EL; ++e) part[(rt * S::EL + e) * 64 + lane] = x.at(mq, e);
+                    if (g == 0) {
+                        float* ml = part + S::ROWS * S::DP + (rt * RL + n) * 2;
+                        ml[0] = x.m[mq];
+                        ml[1] = x.l[mq];
+                    }
+                }
+            }
+            if (!whole && tid == 0) ((int*)part)[S::PART - 1] = careful;
+        }
+        // the next item
+        left -= end_tile - tile;
+        tile = 0;
+        if (dealt) {
+            if (!next_dealt()) break;
+        } else if (++rb == sq.nrb) {
+            rb = 0;
+            if (++hk == c.K) {
+                hk = 0;
+                if (left > 0) {
+                    do { sq = uniform(seq_of<S>(p, ++b)); } while (sq.nrb == 0);
+                }
+            }
+        }
+    }
+}
+
+// The partial results of one cut item added up: block y of a launch has the item that
+// stretch y describes, block x a chunk of its row tiles (x runs first, so an item's blocks
+// spread over the chip's XCDs).  The four waves share the partial results and are added up
+// in LDS.
+constexpr int NTJ = 256, NWJ = 4;
+
+template <typename T, typename S>
+__global__ __launch_bounds__(NTJ) void k_packed_join(AttnArgs p) {
+    constexpr int EC = S::EC, RL = S::RL;
+    __shared__ float s_o[NWJ][EC][64], s_m[NWJ][RL], s_l[NWJ][RL];
+    __shared__ int s_flag[NWJ];
+    const int* desc = p.desc + 8 * blockIdx.y;
+    const int n = desc[0];
+    if (n == 0) return;
+    const int slot0 = desc[1], b = desc[2], hk = desc[3], rb = desc[4];
+    const int lane = threadIdx.x & 63, row = lane % RL, g = lane / RL;
+    const int wave = uniform(threadIdx.x >> 6), rt = blockIdx.x / S::NB, ch = blockIdx.x % S::NB;
+    const rheo_packed_attention_args& a = p.a;
+    const CacheDev& c = p.c;
+    const Seq sq = seq_of<S>(p, b);
+    const int rows = sq.rows * p.g;
+    if (rb * S::ROWS + rt * RL >= rows) return;
+    const float to2 = a.scale * kLog2e;
+    // (slot0 is the first stretch's, maybe its second; the others' first)
+    const int w0 = slot0 >> 1, ml = S::ROWS * S::DP + (rt * RL + row) * 2;
+    const int oi = (rt * S::EL + ch * EC) * 64 + lane;
+    float m = -INFINITY, l = 0.0f, o[EC];
+    int bad = 0;
+#pragma unroll
+    for (int e = 0; e < EC; ++e) o[e] = 0.0f;
+#pragma unroll 1
+    for (int k = wave; k < n; k += 2 * NWJ) {
+        // two at a time (the second may be there twice, with weight 0)
+        const bool both = k + NWJ < n;
+        const int k1 = both ? k + NWJ : k;
+        const float* q0 = c.part + (int64_t)(k ? 2 * (w0 + k) : slot0) * S::PART;
+        const float* q1 = c.part + (int64_t)(k1 ? 2 * (w0 + k1) : slot0) * S::PART;
+        float y0[EC], y1[EC];
+#pragma unroll
+        for (int e = 0; e < EC; ++e) {
+            y0[e] = q0[oi + 64 * e];
+            y1[e] = q1[oi + 64 * e];
+        }
+        const float m0 = q0[ml], l0 = q0[ml + 1], m1 = both ? q1[ml] : -INFINITY, l1 = q1[ml + 1];
+        bad |= ((const int*)q0)[S::PART - 1] | ((const int*)q1)[S::PART - 1];
+        const float top = fmaxf(m, fmaxf(m0, m1)), ref = ref_of<T>(top, to2);
+        const float f = __builtin_amdgcn_exp2f((m * to2 - kRise<T>) - ref);
+        const float f0 = __builtin_amdgcn_exp2f((m0 * to2 - kRise<T>) - ref);
+        const float f1 = both ? __builtin_amdgcn_exp2f((m1 * to2 - kRise<T>) - ref) : 0.0f;
+        m = top;
+        l = __fmaf_rn(l0, f0, l * f);
+        if (both) l = __fmaf_rn(l1, f1, l);
+#pragma unroll
+        for (int e = 0; e < EC; ++e) {
+            o[e] = __fmaf_rn(y0[e], f0, o[e] * f);
+            if (both) o[e] = __fmaf_rn(y1[e], f1, o[e]);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < EC; ++e) s_o[wave][e][lane] = o[e];
+    if (g == 0) {
+        s_m[wave][row] = m;
+        s_l[wave][row] = l;
+    }
+    if (lane == 0) s_flag[wave] = bad;
+    __syncthreads();
+    if (wave) return;
+    m = -INFINITY;
+    for (int k = 0; k < NWJ; ++k) m = fmaxf(m, s_m[k][row]);
+    const float ref = ref_of<T>(m, to2);
+    l = 0.0f;
+    bad = 0;
+#pragma unroll
+    for (int e = 0; e < EC; ++e) o[e] = 0.0f;
+    for (int k = 0; k < NWJ; ++k) {
+        const float f = __builtin_amdgcn_exp2f((s_m[k][row] * to2 - kRise<T>) - ref);
+        l = __fmaf_rn(s_l[k][row], f, l);
+        bad |= s_flag[k];
+#pragma unroll
+        for (int e = 0; e < EC; ++e) o[e] = __fmaf_rn(s_o[k][e][lane], f, o[e]);
+    }
+    const int r = rb * S::ROWS + rt * RL + row;
+    if (r >= rows) return;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int qi = r / p.g, qh = hk * p.g + r - qi * p.g;
+    const int64_t qrow = (int64_t)b * a.n + qi;
+    T* out = (T*)a.out + qrow * a.out_stride + (int64_t)qh * c.D;
+#pragma unroll
+    for (int e = 0; e < EC; ++e) o[e] *= inv;
+    store_chunk<T, S>(out, g, ch, c.D, o);
+    if (a.lse && g == 0 && ch == 0) a.lse[qrow * c.H + qh] = lse_of<T>(m, l, a.scale);
+    if (bad) add_unfinite<T, S>(p, b, hk, sq, qi, out, g, ch);
+}
+
+namespace {
+
+// Shapes for up to 16, 32, 64, 128 and more rows of an item.
+template <int NB>
+struct Shapes {
+    static constexpr bool W = NB > 4;
+    typedef PShape<NB, false, 1, 4, 2> R1;
+    typedef PShape<NB, false, 2, 4, W ? 1 : 2> R2;
+    typedef PShape<NB, true, 1, 2, W ? 1 : 2> R4;
+    typedef PShape<NB, true, 1, 4, W ? 1 : 2> R8;
+    typedef PShape<NB, true, 1, W ? 4 : 8, 1> R16;
+};
+
+template <typename S>
+size_t part_floats(int units) {
+    return (size_t)units * S::RES * 2 * S::PART;
+}
+
+template <int NB>
+size_t workspace(int units) {
+    typedef Shapes<NB> H;
+    const size_t n[5] = {part_floats<typename H::R1>(units), part_floats<typename H::R2>(units),
+                         part_floats<typename H::R4>(units), part_floats<typename H::R8>(units),
+                         part_floats<typename H::R16>(units)};
+    size_t most = 0;
+    for (size_t x : n) most = x > most ? x : most;
+    return most;
+}
+
+template <typename T, typename S>
+hipError_t start(AttnArgs p, hipStream_t s) {
+    p.groups = p.c.slots * S::RES;
+    // (fewer items than workgroups: the cuts are what fills them)
+    p.whole = (int64_t)p.a.n * p.g <= S::ROWS && p.c.B <= kDealt &&
+              (int64_t)p.c.B * p.c.K >= p.groups;
+    k_packed_attention<T, S><<<p.groups, S::NT, S::LDS, s>>>(p);
+    k_packed_join<T, S><<<dim3(S::ROWS / S::RL * S::NB, p.groups), NTJ, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+template <typename T, int NB>
+hipError_t start_rows(const AttnArgs& p, hipStream_t s) {
+    typedef Shapes<NB> H;
+    const int64_t rows = (int64_t)p.a.n * p.g;
+    if (rows <= 16) return start<T, typename H::R1>(p, s);
+    if (rows <= 32) return start<T, typename H::R2>(p, s);
+    if (rows <= 64) return start<T, typename H::R4>(p, s);
+    if (rows <= 128) return start<T, typename H::R8>(p, s);
+    return start<T, typename H::R16>(p, s);
+}
+
+template <typename T, typename S>
+hipError_t allow_lds() {
+    hipError_t e = hipSuccess;
+    if (S::LDS > 64 * 1024)
+        e = hipFuncSetAttribute((const void*)k_packed_attention<T, S>,
+                                hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+    return e;
+}
+
+template <typename T, int NB>
+hipError_t prepare_rows() {
+    typedef Shapes<NB> H;
+    hipError_t e = allow_lds<T, typename H::R1>();
+    if (e == hipSuccess) e = allow_lds<T, typename H::R2>();
+    if (e == hipSuccess) e = allow_lds<T, typename H::R4>();
+    if (e == hipSuccess) e = allow_lds<T, typename H::R8>();
+    return e == hipSuccess ? allow_lds<T, typename H::R16>() : e;
+}
+
+}  // namespace
+
+// The launches for heads of NB blocks of 32 elements; compiled one or two NB to a source.
+template <int NB>
+struct PackedHeads {
+    static hipError_t prepare(int dtype) {
+        return dtype == RHEO_BF16 ? prepare_rows<__bf16, NB>() : prepare_rows<_Float16, NB>();
+    }
+    // floats of partial results, without the descriptions of the joins
+    static size_t workspace(int units) { return rheo::workspace<NB>(units); }
+    static hipError_t launch(const CacheDev& c, const PackedDev& d, const rheo_packed_attention_args& a,
+                             int* desc, hipStream_t s) {
+        AttnArgs p{};
+        p.c = c;
+        p.p = d;
+        p.a = a;
+        p.g = c.H / c.K;
+        p.desc = desc;
+        return c.dtype == RHEO_BF16 ? start_rows<__bf16, NB>(p, s) : start_rows<_Float16, NB>(p, s);
+    }
+};
+
+}  // namespace rheo
