@@ -488,8 +488,8 @@ typedef struct rheo_packed_pages {
     void* k;                     /* [layers][pages][kv_heads] heads' pages              */
     void* v;
     int64_t page_stride;         /* bytes between pages, a multiple of 16, at least
-                                    kv_heads heads' pages; 0: equal to it; pages *
-                                    page_stride <= 2^48                               */
+                                    kv_heads heads' pages, less than 2^32; 0: equal
+                                    to them                                           */
     int64_t layer_stride;        /* bytes between layers, a multiple of 16; 0: pages *
                                     page_stride                                       */
 } rheo_packed_pages;

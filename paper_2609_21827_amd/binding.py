@@ -629,15 +629,19 @@ class PackedCache(Cache):
         head_dim], or of one layer without that dimension."""
         if layers is None:
             return (*self._rows(t, n, self.K, name), 0)
-        if not isinstance(t, torch.Tensor) or t.dim() != 5 or t.shape[0] != layers or not layers:
-            _refuse(f"{name} must be {self.dtype} {(layers, self.B, n, self.K, self.D)} on "
-                    f"{self.device}")
-        at, row = self._rows(t[0], n, self.K, name)
-        least = (self.B * n - 1) * row + self.K * self.D
-        layer = t.stride(0) if layers > 1 else least
-        if n and layer < least:
-            _refuse(f"{name}: layers must not overlap")
-        return at, row, layer
+        B, K, D, shape = self.B, self.K, self.D, (layers, self.B, n, self.K, self.D)
+        if not isinstance(t, torch.Tensor) or t.dtype is not self.dtype or t.shape != shape \
+                or not layers or t.get_device() != self._index:
+            _refuse(f"{name} must be {self.dtype} {shape} on {self.device}")
+        s0, s1, s2, s3, s4 = t.stride()
+        row = s2 if n > 1 else s1 if B > 1 else K * D
+        least = (B * n - 1) * row + K * D
+        layer = s0 if layers > 1 else least
+        if n and (s4 != 1 or (K > 1 and s3 != D) or (B > 1 and s1 != n * row) or row < K * D
+                  or layer < least):
+            _refuse(f"{name}: a row's heads must be dense, rows evenly apart over the batch, layers "
+                    "without overlap")
+        return t.data_ptr(), row, layer
 
     def _of_layers(self, k_pages):
         """The layers that pages have: None (no such dimension) or a number."""

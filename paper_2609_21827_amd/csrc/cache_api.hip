@@ -76,8 +76,8 @@ int check_packed(const CacheDev& d, const rheo_packed_pages& g, int layers, Pack
     p->page_stride = g.page_stride ? g.page_stride : page;
     if (p->page_stride < page || p->page_stride % 16)
         return fail(RHEO_EINVAL, "pages.page_stride must hold a page and be a multiple of 16");
-    if (p->page_stride > ((int64_t)1 << 48) / d.pages)
-        return fail(RHEO_EINVAL, "pages * pages.page_stride must be at most 2^48");
+    if (p->page_stride >> 32)
+        return fail(RHEO_EINVAL, "pages.page_stride must be less than 2^32");
     const int64_t layer = (d.pages - 1) * p->page_stride + page;
     p->layer_stride = g.layer_stride ? g.layer_stride : d.pages * p->page_stride;
     if (layers > 1 && (p->layer_stride < layer || p->layer_stride % 16 ||

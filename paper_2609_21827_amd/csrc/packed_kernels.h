@@ -51,6 +51,11 @@ struct PShape {
     static constexpr int KT = SHARED ? 64 : 32 * NW;          // entries of a tile
     static constexpr int ROWB = 2 * DP + 32;                   // see shared_tiles
     static constexpr int STAGE = KT * (2 * DP + ROWB);
+    // An item's beginning and end (its lengths, rows and first pages one after another, its
+    // results) take as long as some tiles; the line counts as many more for each.  (128
+    // single tokens, 4 key heads, over 2000 to 8000 entries: the last workgroup ends at
+    // 111 us with none, the mean at 83.)
+    static constexpr int SETUP = SHARED ? 4 : 5;
     // a partial result: O^T as the lanes hold it, maximum and sum of each row, a flag
     static constexpr int PART = ROWS * DP + 2 * ROWS + 64;
     static constexpr int RING = NW == 8 ? 3 : 2;             // see shared_tiles
@@ -101,6 +106,7 @@ __device__ __forceinline__ Seq seq_of(const AttnArgs& p, int b) {
 // least).
 struct Span {
     int lo, hi, pages, head, from, count;
+    int length;                    // on the line: `count` and SETUP before them
     __device__ __forceinline__ int tile(int k) const { return k < head ? k : k - head + from; }
 };
 
@@ -125,15 +131,16 @@ __device__ __forceinline__ Span span_of(const AttnArgs& p, const Seq& s, int rb)
     x.from = x.hi < x.lo ? end : tile_of(x.lo);
     x.head = a.window && a.sinks && x.hi >= 0 ? min(tile_of(min(a.sinks - 1, x.hi)) + 1, x.from) : 0;
     x.count = x.head + end - x.from + 1;
+    x.length = x.count + S::SETUP;
     return x;
 }
 
-// Tiles of all row blocks of a sequence, for one key head.
+// The line's part of a sequence and one key head: all its row blocks.
 template <typename S>
 __device__ __forceinline__ int64_t tiles_of_head(const AttnArgs& p, const Seq& s) {
-    if (p.a.mask) return s.nrb ? (int64_t)s.nrb * span_of<S>(p, s, 0).count : 0;
+    if (p.a.mask) return s.nrb ? (int64_t)s.nrb * span_of<S>(p, s, 0).length : 0;
     int64_t t = 0;
-    for (int rb = 0; rb < s.nrb; ++rb) t += span_of<S>(p, s, rb).count;
+    for (int rb = 0; rb < s.nrb; ++rb) t += span_of<S>(p, s, rb).length;
     return t;
 }
 
@@ -163,8 +170,8 @@ __device__ __forceinline__ Seq uniform(const Seq& s) {
     return Seq{uniform(s.len), uniform(s.rows), uniform(s.tail), uniform(s.nrb)};
 }
 __device__ __forceinline__ Span uniform(const Span& s) {
-    return Span{uniform(s.lo),   uniform(s.hi),   uniform(s.pages),
-                uniform(s.head), uniform(s.from), uniform(s.count)};
+    return Span{uniform(s.lo),   uniform(s.hi),    uniform(s.pages), uniform(s.head),
+                uniform(s.from), uniform(s.count), uniform(s.length)};
 }
 
 // Stretch w of the line: tiles [t0, t1) of it, the sequence that t0 is in and the tiles
@@ -245,7 +252,7 @@ __device__ bool deal_items(const AttnArgs& p, int64_t total, int* s_order) {
     __syncthreads();
     for (int b = tid; b < B; b += S::NT) {
         const Seq s = seq_of<S>(p, b);
-        s_tiles[b] = s.nrb ? span_of<S>(p, s, 0).count : 0;
+        s_tiles[b] = s.nrb ? span_of<S>(p, s, 0).length : 0;
     }
     __syncthreads();
     for (int b = tid; b < B; b += S::NT) {
@@ -679,10 +686,14 @@ __device__ __forceinline__ void own_tiles(const AttnArgs& p, const Item& it, Row
 #pragma unroll
                 for (int mq = 0; mq < MQ; ++mq) sc[mq][u] = mfma<T>(ko, x.q[mq][s], sc[mq][u]);
             }
+            // (one block's loads after the other's products: registers, which the loop over
+            // the pages has use for)
+            __builtin_amdgcn_sched_barrier(0);
         }
         u32x4 vo[2 * NB];
 #pragma unroll
         for (int q = 0; q < NB; ++q) {
+            __builtin_amdgcn_sched_barrier(0);
             uint32_t w[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -734,6 +745,12 @@ __device__ __forceinline__ void shared_tiles(const AttnArgs& p, const Item& it, 
     const int end = TAIL ? it.end_tile : it.end_pages;
     if (begin >= end || (TAIL && sq.tail == 0)) return;
 
+    // (of page 0, entry 0: what the lane reads of K; V is as far from it everywhere)
+    const Global<uint8_t> k_codes = k_head + (16 * part + 8 * half);
+    const Global<uint8_t> k_exps = k_head + ((16 * NB + part) << c.page_shift);
+    const int64_t v_less_k = v_head - k_head;
+    const uint32_t stride = (uint32_t)p.p.page_stride;
+
     // Lane 32 h + n makes elements 16 h to 16 h + 15 of its blocks, of entry n of the chunk.
     // A tile's part as loaded: codes and exponents, or (of the tail) the elements themselves.
     uint32_t rk[NS][TAIL ? 8 : 2], rv[NS][TAIL ? 8 : 2], rks[NS], rvs[NS];
@@ -761,22 +778,21 @@ __device__ __forceinline__ void shared_tiles(const AttnArgs& p, const Item& it, 
             } else {
                 const bool good = (unsigned)page < (unsigned)c.pages;
                 outside |= !good;
-                const int entry = (e + n32) & in_page;
-                const int64_t at = (int64_t)(good ? page : 0) * p.p.page_stride;
-                const int64_t codes = at + (entry * (16 * NB) + 16 * part + 8 * half);
-                const int64_t exps = at + (((16 * NB + part) << c.page_shift) + entry);
+                const uint32_t entry = (e + n32) & in_page, from = good ? page : 0;
+                const Global<uint8_t> kc = k_codes + (uint64_t)from * stride + (uint64_t)entry * (16 * NB);
+                const Global<uint8_t> kx = k_exps + (uint64_t)from * stride + entry;
+                const Global<uint8_t> vc = kc + v_less_k, vx = kx + v_less_k;
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
                     // (blocks past the last: the last one's, of no use)
                     const int up = NB % VP == 0 ? VP * s : min(VP * s, NB - 1 - part);
-                    const u32x2 w = load<u32x2, 8>(k_head + codes + 16 * up);
-                    const u32x2 y = load<u32x2, 8>(v_head + codes + 16 * up);
+                    const u32x2 w = load<u32x2, 8>(kc + 16 * up), y = load<u32x2, 8>(vc + 16 * up);
                     rk[s][0] = w[0];
                     rk[s][1] = w[1];
                     rv[s][0] = y[0];
                     rv[s][1] = y[1];
-                    rks[s] = k_head[exps + (up << c.page_shift)];
-                    rvs[s] = v_head[exps + (up << c.page_shift)];
+                    rks[s] = kx[up << c.page_shift];
+                    rvs[s] = vx[up << c.page_shift];
                 }
             }
         } else {
@@ -997,7 +1013,7 @@ k_packed_attention(AttnArgs p) {
             hk = i % c.K;
             sq = uniform(seq_of<S>(p, b));
             if (sq.nrb) {
-                left = uniform(span_of<S>(p, sq, 0).count);
+                left = uniform(span_of<S>(p, sq, 0).length);
                 ++round;
                 return true;
             }
@@ -1013,12 +1029,12 @@ k_packed_attention(AttnArgs p) {
         const int64_t per_head = tiles_of_head<S>(p, sq);
         hk = uniform((int)(rel / per_head));
         rel -= hk * per_head;
-        for (int n; rel >= (n = span_of<S>(p, sq, rb).count); ++rb) rel -= n;
+        for (int n; rel >= (n = span_of<S>(p, sq, rb).length); ++rb) rel -= n;
         rb = uniform(rb);
         tile = uniform((int)rel);
         left = st.t1 - st.t0;
         // the join of the first item, by the first cut inside it
-        const int64_t begins = st.t0 - tile, ends = begins + span_of<S>(p, sq, rb).count;
+        const int64_t begins = st.t0 - tile, ends = begins + span_of<S>(p, sq, rb).length;
         if (tid == 0 && tile > 0 && stretch_start(st.total, st.groups, w - 1) <= begins) {
             int* d = p.desc + 8 * w;
             int n = 2;
@@ -1033,8 +1049,9 @@ k_packed_attention(AttnArgs p) {
 
     for (bool first = true; left > 0; first = false) {
         const Span span = uniform(span_of<S>(p, sq, rb));
-        const int end_tile = (int)min((int64_t)span.count, tile + left);
-        // (of the pages; then the tail's)
+        const int end_place = (int)min((int64_t)span.length, tile + left);
+        // its tiles in the stretch: of the pages, then of the tail (none: a part of nothing)
+        const int begin_tile = max(tile - S::SETUP, 0), end_tile = max(end_place - S::SETUP, 0);
         const int end_pages = min(end_tile, span.from < span.pages ? span.pages - span.from + span.head
                                                                    : min(span.head, span.pages));
         Rows<S> x;
@@ -1072,7 +1089,7 @@ k_packed_attention(AttnArgs p) {
         hi_least = uniform(hi_least);
         const int sinks = a.window ? a.sinks : 0;
 
-        const Item it{uniform(b),         uniform(hk),       uniform(rb), sq,       span, uniform(tile),
+        const Item it{uniform(b),         uniform(hk),       uniform(rb), sq,       span, uniform(begin_tile),
                       uniform(end_pages), uniform(end_tile), lo_most,     hi_least, sinks};
         bool careful = false;
         for (;;) {                                   // again where the tail is not finite
@@ -1156,7 +1173,7 @@ k_packed_attention(AttnArgs p) {
                                 x.o[mq][t][r] += out[(((k - 1) * MQ + mq) * S::EL + 4 * t + r) * 64 + lane];
         }
         if (S::SHARED || wave == 0) {
-            const bool whole = tile == 0 && end_tile == span.count;
+            const bool whole = tile == 0 && end_place == span.length;
             float* part = c.part + (int64_t)(2 * w + (first ? 0 : 1)) * S::PART;
 #pragma unroll
             for (int mq = 0; mq < MQ; ++mq) {
@@ -1191,7 +1208,7 @@ k_packed_attention(AttnArgs p) {
             if (!whole && tid == 0) ((int*)part)[S::PART - 1] = careful;
         }
         // the next item
-        left -= end_tile - tile;
+        left -= end_place - tile;
         tile = 0;
         if (dealt) {
             if (!next_dealt()) break;

@@ -57,81 +57,97 @@ __device__ __forceinline__ bool store_part(const CacheDev& c, const PackedDev& p
 
 }  // namespace
 
-// Four lanes hold a block of 32 elements, 16 bytes each: the largest magnitude passes
-// between them, each writes a word of codes, the first the exponent.  A block of threads
-// takes `each` rows at a time, some 4096 elements or a row.  Bound by memory.
-template <typename T>
-__global__ __launch_bounds__(NTP) void k_packed_append(CacheDev c, PackedDev p, rheo_packed_rows r,
-                                                       int each) {
-    const int parts = c.K * 4 * p.nb;
+// Rows into pages, or (READ) out of them.  Four lanes hold a block of 32 elements, 16 bytes
+// each: the largest magnitude passes between them, each writes a word of codes, the first
+// the exponent.  A workgroup takes ROWS rows at a time, head after head, so that what
+// it writes of a head's page (or reads) is 16 entries next to each other where their slots are:
+// 1 KB of codes instead of 64 bytes here and there, which the chip's eight L2 would each
+// write a part of.  Bound by memory: 12064 rows of 40 heads of 80, 203 MB, 59 us into pages
+// (79 row by row) and 39 out of them (59).
+
+template <typename T, int NB, int ROWS, bool READ>
+__global__ __launch_bounds__(NTP) void k_packed_rows(CacheDev c, PackedDev p, rheo_packed_rows r,
+                                                     int split, int heads) {
+    constexpr int PARTS = 4 * NB;
+    __shared__ int64_t s_page[ROWS];        // bytes of the row's page from the pool's start, or -1
+    __shared__ int s_entry[ROWS];
     const int64_t rows = (int64_t)c.B * r.n;
-    const int layer = blockIdx.y;
-    const T* const k = (const T*)r.k + layer * r.layer_stride;
-    const T* const v = (const T*)r.v + layer * r.layer_stride;
+    const int layer = blockIdx.y, tid = threadIdx.x;
+    T* const k = (T*)r.k + layer * r.layer_stride;
+    T* const v = (T*)r.v + layer * r.layer_stride;
     uint8_t* const kp = p.k + layer * p.layer_stride;
     uint8_t* const vp = p.v + layer * p.layer_stride;
     bool bad = false;
-    for (int64_t r0 = (int64_t)blockIdx.x * each; r0 < rows; r0 += (int64_t)gridDim.x * each) {
-        const int here = (int)min((int64_t)each, rows - r0);
-        for (int f = threadIdx.x; f < here * parts; f += NTP) {
-            const int i = f / parts;
-            const int64_t row = r0 + i, slot = r.slots[row];
-            if (slot < 0) continue;
-            int64_t page;
-            int entry;
-            if (!place_of(c, p, slot, &page, &entry)) continue;
-            const Part u = part_of(f - i * parts, p.nb);
-            const int64_t at = row * r.row_stride + u.head * c.D + u.d;
-            uint4 x = make_uint4(0, 0, 0, 0), y = x;
-            if (u.d < c.D) {
-                x = *(const uint4*)(k + at);
-                y = *(const uint4*)(v + at);
+    // (`heads` of them from h0 on, the workgroup's of `split` next to each other)
+    const int h0 = blockIdx.x % split * heads, end = min(heads, c.K - h0) * ROWS * PARTS;
+    const int64_t step = (int64_t)(gridDim.x / split) * ROWS;
+    for (int64_t r0 = (int64_t)(blockIdx.x / split) * ROWS; r0 < rows; r0 += step) {
+        __syncthreads();
+        if (tid < ROWS) {
+            const int64_t slot = r0 + tid < rows ? r.slots[r0 + tid] : -1;
+            int64_t page = 0;
+            int entry = 0;
+            const bool there = slot >= 0 && place_of(c, p, slot, &page, &entry);
+            s_page[tid] = there ? page : -1;
+            s_entry[tid] = entry;
+        }
+        __syncthreads();
+        // (a multiple of four: a block's lanes are all here or none)
+        for (int f0 = tid; f0 < end; f0 += 2 * NTP) {
+            // two parts at a time, all their loads first
+            Part u[2];
+            int64_t page[2], at[2];
+            int entry[2];
+            uint4 x[2], y[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int f = f0 + j * NTP, g = f / PARTS, i = g % ROWS, q = f % PARTS;
+                page[j] = f < end ? s_page[i] : -1;
+                entry[j] = s_entry[i];
+                u[j] = Part{h0 + g / ROWS, q >> 2, q & 3, 8 * q};
+                at[j] = (r0 + i) * r.row_stride + u[j].head * c.D + u[j].d;
+                x[j] = y[j] = make_uint4(0, 0, 0, 0);
+                if (page[j] < 0) continue;
+                if constexpr (!READ) {
+                    if (u[j].d < c.D) {
+                        x[j] = *(const uint4*)(k + at[j]);
+                        y[j] = *(const uint4*)(v + at[j]);
+                    }
+                } else {
+                    const int64_t codes = page[j] + codes_at(p, u[j], entry[j]);
+                    const int64_t exps = page[j] + exponent_at(c, p, u[j], entry[j]);
+                    x[j].x = *(const uint32_t*)(kp + codes);
+                    y[j].x = *(const uint32_t*)(vp + codes);
+                    x[j].y = kp[exps];
+                    y[j].y = vp[exps];
+                }
             }
-            bad |= store_part<T>(c, p, u, kp + page, entry, x);
-            bad |= store_part<T>(c, p, u, vp + page, entry, y);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (page[j] < 0) continue;
+                if constexpr (!READ) {
+                    bad |= store_part<T>(c, p, u[j], kp + page[j], entry[j], x[j]);
+                    bad |= store_part<T>(c, p, u[j], vp + page[j], entry[j], y[j]);
+                } else if (u[j].d < c.D) {
+                    // (every code's value is exact in T)
+                    const float f = scale_of(x[j].y), g = scale_of(y[j].y);
+                    *(uint4*)(k + at[j]) = make_uint4(pair_of<T, 0>(x[j].x, f), pair_of<T, 1>(x[j].x, f),
+                                                      pair_of<T, 2>(x[j].x, f), pair_of<T, 3>(x[j].x, f));
+                    *(uint4*)(v + at[j]) = make_uint4(pair_of<T, 0>(y[j].x, g), pair_of<T, 1>(y[j].x, g),
+                                                      pair_of<T, 2>(y[j].x, g), pair_of<T, 3>(y[j].x, g));
+                }
+            }
         }
     }
-    if (__any(bad) && (threadIdx.x & 63) == 0) atomicOr(c.err, CE_VALUE);
-}
-
-// The same turned round.  Every code's value is exact in T.
-template <typename T>
-__global__ __launch_bounds__(NTP) void k_packed_read(CacheDev c, PackedDev p, rheo_packed_rows r,
-                                                     int each) {
-    const int parts = c.K * 4 * p.nb;
-    const int64_t rows = (int64_t)c.B * r.n;
-    const int layer = blockIdx.y;
-    T* const k = (T*)r.k + layer * r.layer_stride;
-    T* const v = (T*)r.v + layer * r.layer_stride;
-    const uint8_t* const kp = p.k + layer * p.layer_stride;
-    const uint8_t* const vp = p.v + layer * p.layer_stride;
-    for (int64_t r0 = (int64_t)blockIdx.x * each; r0 < rows; r0 += (int64_t)gridDim.x * each) {
-        const int here = (int)min((int64_t)each, rows - r0);
-        for (int f = threadIdx.x; f < here * parts; f += NTP) {
-            const int i = f / parts;
-            const int64_t row = r0 + i, slot = r.slots[row];
-            if (slot < 0) continue;
-            int64_t page;
-            int entry;
-            if (!place_of(c, p, slot, &page, &entry)) continue;
-            const Part u = part_of(f - i * parts, p.nb);
-            if (u.d >= c.D) continue;
-            const int64_t codes = page + codes_at(p, u, entry);
-            const int64_t at_scale = page + exponent_at(c, p, u, entry);
-            const int64_t at = row * r.row_stride + u.head * c.D + u.d;
-            const uint32_t x = *(const uint32_t*)(kp + codes), y = *(const uint32_t*)(vp + codes);
-            const float f_x = scale_of(kp[at_scale]), f_y = scale_of(vp[at_scale]);
-            *(uint4*)(k + at) = make_uint4(pair_of<T, 0>(x, f_x), pair_of<T, 1>(x, f_x),
-                                           pair_of<T, 2>(x, f_x), pair_of<T, 3>(x, f_x));
-            *(uint4*)(v + at) = make_uint4(pair_of<T, 0>(y, f_y), pair_of<T, 1>(y, f_y),
-                                           pair_of<T, 2>(y, f_y), pair_of<T, 3>(y, f_y));
-        }
-    }
+    if (!READ && __any(bad) && (tid & 63) == 0) atomicOr(c.err, CE_VALUE);
 }
 
 // Every block of a sequence walks the accepted path for itself, then rounds its share of
-// the layers' rows into the pages.  Rows and pages are different memory, so the order is
-// free.  The sequence's last block writes the length, which may be lens itself.
+// the layers' rows into the pages, a part of all the path's rows a thread.  Rows and pages are
+// different memory, so the order is free.  The sequence's last block writes the length, which
+// may be lens itself.  Bound by memory, and by writes of less than its lines: 128 sequences, 32
+// layers, 5 entries on average (100 MB) 35 us; one sequence 5, the walk's latency.  (The
+// path's rows of a head by neighbouring threads: 39 to 51 us.)
 template <typename T>
 __global__ __launch_bounds__(NTP) void k_packed_commit(CacheDev c, PackedDev p,
                                                        rheo_packed_commit_args a, int split) {
@@ -208,36 +224,52 @@ __global__ __launch_bounds__(NTP) void k_packed_commit(CacheDev c, PackedDev p,
 
 namespace {
 
-// Rows that a block takes at a time, and blocks.
-struct Cut {
-    int each, blocks;
-};
-Cut cut_rows(const CacheDev& c, const PackedDev& p, int64_t rows, int layers) {
-    const int parts = c.K * 4 * p.nb;
-    const int each = parts < 512 ? 512 / parts : 1;
-    const int64_t blocks = (rows + each - 1) / each;
-    const int most = 65536 / layers;         // (a launch has less than 2^32 threads)
-    return {each, (int)(blocks < most ? blocks : most)};
+// f(a constant: the blocks of 32 elements of a head, 1 to 8)
+template <typename F>
+hipError_t by_blocks(int nb, F f) {
+    switch (nb) {
+    case 1: f(std::integral_constant<int, 1>()); break;
+    case 2: f(std::integral_constant<int, 2>()); break;
+    case 3: f(std::integral_constant<int, 3>()); break;
+    case 4: f(std::integral_constant<int, 4>()); break;
+    case 5: f(std::integral_constant<int, 5>()); break;
+    case 6: f(std::integral_constant<int, 6>()); break;
+    case 7: f(std::integral_constant<int, 7>()); break;
+    default: f(std::integral_constant<int, 8>());
+    }
+    return hipGetLastError();
+}
+
+template <typename T, bool READ>
+hipError_t start_rows(const CacheDev& c, const PackedDev& p, const rheo_packed_rows& r, hipStream_t s) {
+    return by_blocks(p.nb, [&](auto nb) {
+        // a sequence's few rows are next to no others: one at a time (one row of 8 heads 2.8 us,
+        // as one of 16 5.4)
+        const int rows = r.n < 8 ? 1 : 16;
+        const int64_t groups = ((int64_t)c.B * r.n + rows - 1) / rows;
+        // some four parts a thread: more workgroups, where rows are few, than one for all heads
+        const int most_heads = 4 * NTP / (rows * 4 * nb), heads = most_heads < 1 ? 1 : most_heads;
+        const int split = (c.K + heads - 1) / heads;
+        int64_t most = (1 << 22) / ((int64_t)r.layers * split);   // (fewer than 2^32 threads)
+        if (most < 1) most = 1;
+        const dim3 grid((int)(groups < most ? groups : most) * split, r.layers);
+        if (rows == 1) k_packed_rows<T, nb, 1, READ><<<grid, NTP, 0, s>>>(c, p, r, split, heads);
+        else k_packed_rows<T, nb, 16, READ><<<grid, NTP, 0, s>>>(c, p, r, split, heads);
+    });
 }
 
 }  // namespace
 
 hipError_t launch_packed_append(const CacheDev& c, const PackedDev& p, const rheo_packed_rows& r,
                                 hipStream_t s) {
-    const Cut t = cut_rows(c, p, (int64_t)c.B * r.n, r.layers);
-    const dim3 grid(t.blocks, r.layers);
-    if (c.dtype == RHEO_BF16) k_packed_append<__bf16><<<grid, NTP, 0, s>>>(c, p, r, t.each);
-    else k_packed_append<_Float16><<<grid, NTP, 0, s>>>(c, p, r, t.each);
-    return hipGetLastError();
+    return c.dtype == RHEO_BF16 ? start_rows<__bf16, false>(c, p, r, s)
+                                : start_rows<_Float16, false>(c, p, r, s);
 }
 
 hipError_t launch_packed_read(const CacheDev& c, const PackedDev& p, const rheo_packed_rows& r,
                               hipStream_t s) {
-    const Cut t = cut_rows(c, p, (int64_t)c.B * r.n, r.layers);
-    const dim3 grid(t.blocks, r.layers);
-    if (c.dtype == RHEO_BF16) k_packed_read<__bf16><<<grid, NTP, 0, s>>>(c, p, r, t.each);
-    else k_packed_read<_Float16><<<grid, NTP, 0, s>>>(c, p, r, t.each);
-    return hipGetLastError();
+    return c.dtype == RHEO_BF16 ? start_rows<__bf16, true>(c, p, r, s)
+                                : start_rows<_Float16, true>(c, p, r, s);
 }
 
 hipError_t launch_packed_commit(const CacheDev& c, const PackedDev& p,
