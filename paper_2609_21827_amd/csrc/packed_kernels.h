@@ -1324,9 +1324,8 @@ namespace {
 template <int NB>
 struct Shapes {
     static constexpr bool W = NB > 4;
-    typedef PShape<NB, false, 1, 4, 2> R1;
-    typedef PShape<NB, false, 2, 4, W ? 1 : 2> R2;
-    typedef PShape<NB, true, 1, 2, W ? 1 : 2> R4;
+    typedef PShape<NB, false, 1, 4, W ? 1 : 2> R1;
+    typedef PShape<NB, true, 1, W ? 4 : 2, W ? 1 : 2> R4;
     typedef PShape<NB, true, 1, 4, W ? 1 : 2> R8;
     typedef PShape<NB, true, 1, W ? 4 : 8, 1> R16;
 };
@@ -1339,9 +1338,8 @@ size_t part_floats(int units) {
 template <int NB>
 size_t workspace(int units) {
     typedef Shapes<NB> H;
-    const size_t n[5] = {part_floats<typename H::R1>(units), part_floats<typename H::R2>(units),
-                         part_floats<typename H::R4>(units), part_floats<typename H::R8>(units),
-                         part_floats<typename H::R16>(units)};
+    const size_t n[4] = {part_floats<typename H::R1>(units), part_floats<typename H::R4>(units),
+                         part_floats<typename H::R8>(units), part_floats<typename H::R16>(units)};
     size_t most = 0;
     for (size_t x : n) most = x > most ? x : most;
     return most;
@@ -1363,7 +1361,6 @@ hipError_t start_rows(const AttnArgs& p, hipStream_t s) {
     typedef Shapes<NB> H;
     const int64_t rows = (int64_t)p.a.n * p.g;
     if (rows <= 16) return start<T, typename H::R1>(p, s);
-    if (rows <= 32) return start<T, typename H::R2>(p, s);
     if (rows <= 64) return start<T, typename H::R4>(p, s);
     if (rows <= 128) return start<T, typename H::R8>(p, s);
     return start<T, typename H::R16>(p, s);
@@ -1382,7 +1379,6 @@ template <typename T, int NB>
 hipError_t prepare_rows() {
     typedef Shapes<NB> H;
     hipError_t e = allow_lds<T, typename H::R1>();
-    if (e == hipSuccess) e = allow_lds<T, typename H::R2>();
     if (e == hipSuccess) e = allow_lds<T, typename H::R4>();
     if (e == hipSuccess) e = allow_lds<T, typename H::R8>();
     return e == hipSuccess ? allow_lds<T, typename H::R16>() : e;
