@@ -31,7 +31,7 @@ auto by_blocks(int nb, F f) {
     }
 }
 
-constexpr size_t kDescs = 4 * 8;         // words a compute unit: two workgroups' joins
+constexpr size_t kDescs = 2 * 8;         // words a compute unit: two workgroups' joins
 
 }  // namespace
 

@@ -3,26 +3,31 @@
 // o_i = sum_j p_ij v_j with p = softmax_j(scale q_i.k_j), in one pass over the entries
 // with a running maximum and sum, for the g = heads / kv_heads query heads of a key head
 // and a sequence's rows together, as rheo_tree_attention does it.  What differs is where
-// the operands come from: a wave reads codes, 17 bytes for 32 elements, and makes the matrix
-// cores' operands of them in its registers (the values are exact in 16 bits), with nothing
-// passing through LDS and no wave waiting for another before an item's end.
+// the operands come from: codes, 17 bytes for 32 elements, whose values (exact in 16 bits) the
+// matrix cores take.  gfx950 makes a word of two of them from a byte in one instruction.
 //
-// Products are transposed, S^T = K Q^T and O^T = V^T P^T, as 16x16x32 tiles; a wave
-// takes 32 entries at a time, two blocks u of 16, and 16 MQ rows.  Lane 16 g + n holds
-//   of K: entry n of each block, elements 8 NB g + 8 s + (0..7) at step s (Q alike), so
-//         that its 4 NB bytes of codes lie together;
-//   of V: elements 2 NB n + (0..2 NB - 1) of the entries 4 g + (0..3) of both blocks;
-//         column n of tile t is element 2 NB n + t, and a tile's operand is the entries'
-//         words of two elements taken apart and joined by pairs of entries;
-//   of S^T: row n, entries 4 g + (0..3) of each block: with the second product's inner
-//         index 8 g + j <-> entry (j < 4 ? 4 g + j of block 0 : 4 g + j - 4 of block 1) its
-//         probabilities are the right operand as they stand;
-//   of O^T: row n, elements 8 NB g + (0..8 NB - 1), next to each other.
+// Products are transposed, S^T = K Q^T and O^T = V^T P^T, so that a lane's scores are all one
+// row's and its probabilities are the second product's right operand as they stand.  Up to 16 rows
+// each wave makes its operands in registers (own_tiles), 16x16x32; more rows take them
+// from LDS, where all waves put them (shared_tiles), 32x32x16.
 //
 // Work is one line of tiles over all (sequence, key head, block of rows), cut evenly over
 // the workgroups; items that are cut leave partial results, which k_packed_join adds up.
 // With a window an item's tiles are those of the first entries that stay visible and those
 // from the first row's window on.
+//
+// What bounds it.  Few rows, memory: 128 single tokens over 2000 to 8191 entries (4 key heads
+// of 128, fp16, 358 MB) 98 us where a copy's rate would take 72; what is over is the line, the
+// items' beginnings one after another, and some workgroups' slower memory.  Up to 256 rows,
+// issuing instructions: 64 trees of 244 rows over 1000 to 4096 entries (8 key heads, 0.27 GB,
+// 176 GFLOP) 212 us, 830 TFLOP/s, where a large product's rate would take 152.  A SIMD's two
+// waves have 2160 cycles of products a tile of 64 entries and 560 vector operations, each 4.6
+// cycles (measured beside products: 6 + 4.6 n a product of 16.9); one wave's chain alone is
+// some 3150 cycles, and the tile takes 4900.  No gain came from one of the two waves half a
+// tile later (211 to 237 us), from their priorities, from loads two tiles ahead, or from a
+// chunk's scores one chunk ahead (registers spill: 1624 us).  Scores by the matrix cores' own
+// 4-bit operands (K as it is, q in two parts of 8 bits) are no faster, and off by 2^-16 of the
+// sum of |q k|.
 #pragma once
 
 #include <type_traits>
@@ -36,30 +41,30 @@ namespace {
 
 // A launch's shape: NB blocks of 32 head elements, a workgroup of NW waves, RES of them to a
 // compute unit.  SHARED: the waves have 32 rows each and make a tile's operands together, in
-// LDS (shared_tiles), 64 entries of it.  Else all have the same 16 MQ rows and every
-// fourth 32 entries (own_tiles).
-template <int NB_, bool SHARED_, int MQ_, int NW_, int RES_>
+// LDS (shared_tiles), 64 entries of it.  Else all have the same 16 rows and every fourth 32
+// entries (own_tiles).
+template <int NB_, bool SHARED_, int NW_, int RES_>
 struct PShape {
     static constexpr bool SHARED = SHARED_;
-    static constexpr int NB = NB_, MQ = MQ_, NW = NW_, RES = RES_;
+    static constexpr int NB = NB_, NW = NW_, RES = RES_;
     static constexpr int DP = 32 * NB, NT = 64 * NW;
     static constexpr int WAVES = (RES * NW + 3) / 4;           // a SIMD
-    static constexpr int RL = SHARED ? 32 : 16;                // rows of a wave's tile: n of a lane,
+    static constexpr int RL = SHARED ? 32 : 16;                // rows of a wave: n of a lane
     static constexpr int EL = RL * DP / 64;                    // elements of one that a lane holds
     static constexpr int EC = EL / NB;                         // ... in a chunk of them
-    static constexpr int ROWS = RL * MQ * (SHARED ? NW : 1);   // of an item
+    static constexpr int ROWS = RL * (SHARED ? NW : 1);         // of an item
     static constexpr int KT = SHARED ? 64 : 32 * NW;          // entries of a tile
     static constexpr int ROWB = 2 * DP + 32;                   // see shared_tiles
     static constexpr int STAGE = KT * (2 * DP + ROWB);
     // An item's beginning and end (its lengths, rows and first pages one after another, its
-    // results) take as long as some tiles; the line counts as many more for each.  (128
+    // results) take as long as some tiles: the line counts as many more for each.  (128
     // single tokens, 4 key heads, over 2000 to 8000 entries: the last workgroup ends at
     // 111 us with none, the mean at 83.)
     static constexpr int SETUP = SHARED ? 4 : 5;
     // a partial result: O^T as the lanes hold it, maximum and sum of each row, a flag
     static constexpr int PART = ROWS * DP + 2 * ROWS + 64;
     static constexpr int RING = NW == 8 ? 3 : 2;             // see shared_tiles
-    static constexpr int LDS = SHARED ? RING * STAGE : (NW - 1) * MQ * EL * 64 * 4;
+    static constexpr int LDS = SHARED ? RING * STAGE : (NW - 1) * EL * 64 * 4;
     // Element e of a lane's EL, of the lanes' group g (see the mappings above)
     __device__ __forceinline__ static int element(int g, int e) {
         return SHARED ? 32 * (e / 16) + 8 * (e % 16 / 4) + 4 * g + e % 4
@@ -106,12 +111,12 @@ __device__ __forceinline__ Seq seq_of(const AttnArgs& p, int b) {
 // least).
 struct Span {
     int lo, hi, pages, head, from, count;
-    int length;                    // on the line: `count` and SETUP before them
+    int length;                    // on the line: `count` and `setup` before them
     __device__ __forceinline__ int tile(int k) const { return k < head ? k : k - head + from; }
 };
 
 template <typename S>
-__device__ __forceinline__ Span span_of(const AttnArgs& p, const Seq& s, int rb) {
+__device__ __forceinline__ Span span_of(const AttnArgs& p, const Seq& s, int rb, int setup = 0) {
     const rheo_packed_attention_args& a = p.a;
     Span x;
     x.hi = s.len + s.tail - 1;
@@ -131,16 +136,16 @@ __device__ __forceinline__ Span span_of(const AttnArgs& p, const Seq& s, int rb)
     x.from = x.hi < x.lo ? end : tile_of(x.lo);
     x.head = a.window && a.sinks && x.hi >= 0 ? min(tile_of(min(a.sinks - 1, x.hi)) + 1, x.from) : 0;
     x.count = x.head + end - x.from + 1;
-    x.length = x.count + S::SETUP;
+    x.length = x.count + setup;
     return x;
 }
 
 // The line's part of a sequence and one key head: all its row blocks.
 template <typename S>
-__device__ __forceinline__ int64_t tiles_of_head(const AttnArgs& p, const Seq& s) {
-    if (p.a.mask) return s.nrb ? (int64_t)s.nrb * span_of<S>(p, s, 0).length : 0;
+__device__ __forceinline__ int64_t length_of_head(const AttnArgs& p, const Seq& s, int setup) {
+    if (p.a.mask) return s.nrb ? (int64_t)s.nrb * span_of<S>(p, s, 0, setup).length : 0;
     int64_t t = 0;
-    for (int rb = 0; rb < s.nrb; ++rb) t += span_of<S>(p, s, rb).length;
+    for (int rb = 0; rb < s.nrb; ++rb) t += span_of<S>(p, s, rb, setup).length;
     return t;
 }
 
@@ -149,12 +154,6 @@ template <typename T>
 using Global = const __attribute__((address_space(1))) T*;
 template <typename T>
 __device__ __forceinline__ Global<T> global(const void* q) { return (Global<T>)(const T*)q; }
-// ... that the kernel does not write, of addresses that are the same in all lanes: these go
-// through the scalar cache.
-template <typename T>
-using Constant = const __attribute__((address_space(4))) T*;
-template <typename T>
-__device__ __forceinline__ Constant<T> constant(const void* q) { return (Constant<T>)(uintptr_t)q; }
 template <typename T, int A>
 __device__ __forceinline__ T load(Global<uint8_t> q) {
     struct __attribute__((packed, aligned(A))) Word { T v; };
@@ -178,35 +177,66 @@ __device__ __forceinline__ Span uniform(const Span& s) {
 // before that sequence.  All threads of the block call it.
 struct Stretch {
     int64_t total, t0, t1, before;
-    int groups, seq;
+    int groups, seq, setup;        // (setup: see SETUP; what an item's length has of it)
+    Seq of;                        // that sequence's
 };
 
+// a / b of numbers that are seldom past 32 bits (a 64-bit division is some hundred
+// instructions, one after another)
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    if (((uint64_t)a | (uint64_t)b) >> 32) return a / b;
+    return (uint32_t)a / (uint32_t)b;
+}
+
 __device__ __forceinline__ int64_t stretch_start(int64_t total, int groups, int w) {
-    return total * w / groups;
+    return quotient(total * w, groups);
+}
+// the stretch that place t of the line is in
+__device__ __forceinline__ int stretch_of(int64_t total, int groups, int64_t t) {
+    return (int)quotient((t + 1) * groups - 1, total);
 }
 
 template <typename S>
 __device__ Stretch find_stretch(const AttnArgs& p, int w) {
-    __shared__ int64_t s_wave[S::NW], s_before;
+    __shared__ int64_t s_wave[S::NW], s_items[S::NW], s_before;
     __shared__ int s_seq;
+    __shared__ Seq s_of;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, B = p.c.B;
     const int per = (B + S::NT - 1) / S::NT, b0 = min(tid * per, B), b1 = min(b0 + per, B);
-    int64_t mine = 0;
-    for (int b = b0; b < b1; ++b) mine += p.c.K * tiles_of_head<S>(p, seq_of<S>(p, b));
-    int64_t incl = mine;
+    int64_t mine = 0, items = 0;             // tiles and items of the thread's sequences
+    for (int b = b0; b < b1; ++b) {
+        const Seq s = seq_of<S>(p, b);
+        mine += p.c.K * length_of_head<S>(p, s, 0);
+        items += (int64_t)p.c.K * s.nrb;
+    }
+    int64_t incl = mine, incl_items = items;
     for (int o = 1; o < 64; o <<= 1) {
-        const int64_t u = __shfl_up(incl, o);
-        if (lane >= o) incl += u;
+        const int64_t u = __shfl_up(incl, o), v = __shfl_up(incl_items, o);
+        if (lane >= o) {
+            incl += u;
+            incl_items += v;
+        }
     }
-    if (lane == 63) s_wave[wave] = incl;
+    if (lane == 63) {
+        s_wave[wave] = incl;
+        s_items[wave] = incl_items;
+    }
     __syncthreads();
-    int64_t excl = incl - mine, total = 0;
+    int64_t excl = incl - mine, total = 0, excl_items = incl_items - items, all_items = 0;
     for (int v = 0; v < S::NW; ++v) {
-        if (v < wave) excl += s_wave[v];
+        if (v < wave) {
+            excl += s_wave[v];
+            excl_items += s_items[v];
+        }
         total += s_wave[v];
+        all_items += s_items[v];
     }
-    total = uniform64(total);
     Stretch r;
+    // (where every tile can have a workgroup, each begins one item at most)
+    r.setup = uniform(total > p.groups ? S::SETUP : 0);
+    total = uniform64(total + r.setup * all_items);
+    excl += r.setup * excl_items;
+    mine += r.setup * items;
     r.total = total;
     r.groups = (int)(total < p.groups ? total : p.groups);
     r.seq = 0;
@@ -220,9 +250,11 @@ __device__ Stretch find_stretch(const AttnArgs& p, int w) {
     if (r.t0 >= excl && r.t0 < excl + mine) {
         int64_t t = excl;
         for (int b = b0; b < b1; ++b) {
-            const int64_t k = p.c.K * tiles_of_head<S>(p, seq_of<S>(p, b));
+            const Seq s = seq_of<S>(p, b);
+            const int64_t k = p.c.K * length_of_head<S>(p, s, r.setup);
             if (r.t0 < t + k) {
                 s_seq = b;
+                s_of = s;
                 s_before = t;
                 break;
             }
@@ -231,6 +263,7 @@ __device__ Stretch find_stretch(const AttnArgs& p, int w) {
     }
     __syncthreads();
     r.seq = uniform(s_seq);
+    r.of = uniform(s_of);
     r.before = uniform64(s_before);
     return r;
 }
@@ -246,13 +279,13 @@ __device__ __forceinline__ int dealt_item(int round, int w, int groups) {
 }
 
 template <typename S>
-__device__ bool deal_items(const AttnArgs& p, int64_t total, int* s_order) {
+__device__ bool deal_items(const AttnArgs& p, int64_t total, int setup, int* s_order) {
     __shared__ int s_tiles[kDealt], s_most[S::NW];
     const int tid = threadIdx.x, B = p.c.B, K = p.c.K, items = B * K;
     __syncthreads();
     for (int b = tid; b < B; b += S::NT) {
         const Seq s = seq_of<S>(p, b);
-        s_tiles[b] = s.nrb ? span_of<S>(p, s, 0).length : 0;
+        s_tiles[b] = s.nrb ? span_of<S>(p, s, 0, setup).length : 0;
     }
     __syncthreads();
     for (int b = tid; b < B; b += S::NT) {
@@ -280,7 +313,6 @@ __device__ bool deal_items(const AttnArgs& p, int64_t total, int* s_order) {
 }
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -307,16 +339,6 @@ __device__ __forceinline__ f32x4 mfma(const u32x4& a, const u32x4& b, const f32x
                                                       __builtin_bit_cast(v8, b), c, 0, 0, 0);
 }
 
-// A row's maximum or sum over the four lanes that hold it.
-__device__ __forceinline__ float row_max(float x) {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ __forceinline__ float row_sum(float x) {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
-}
-
 // Both elements of a word 0 where they are infinite or NaN.
 template <typename T>
 __device__ __forceinline__ uint32_t finite_pair(uint32_t w) {
@@ -330,47 +352,36 @@ __device__ __forceinline__ int k_block(int g, int s) { return (NB * g + s) >> 2;
 template <int NB>
 __device__ __forceinline__ int v_block(int n, int p) { return (NB * n + p) >> 4; }
 
-// What a wave holds of an item: MQ tiles of RL rows, of which lane RL g + n has row n.
+// What a wave holds of an item: lane RL g + n has row n's.
 template <typename S>
 struct Rows {
     typedef std::conditional_t<S::SHARED, f32x16, f32x4> Part;
     static constexpr int QS = S::SHARED ? 2 * S::NB : S::NB, VL = S::SHARED ? 16 : 4;
-    u32x4 q[S::MQ][QS];
-    Part o[S::MQ][S::EL / VL];
-    float m[S::MQ], l[S::MQ];      // the exponents' reference, a score; the lane's sum
-    int lo[S::MQ], hi[S::MQ];      // entries that the lane's row attends (and sinks)
-    uint32_t mask[S::MQ];          // its row of the mask
-    __device__ __forceinline__ float at(int mq, int e) const { return o[mq][e / VL][e % VL]; }
+    u32x4 q[QS];
+    Part o[S::EL / VL];
+    float m, l;                    // the exponents' reference, a score; the lane's sum
+    int lo, hi;                    // entries that the row attends (and sinks)
+    uint32_t mask;                 // its row of the mask
+    __device__ __forceinline__ float at(int e) const { return o[e / VL][e % VL]; }
 };
 
 // The exponents' reference follows a row's own maximum by steps (kSlack), so that O is
-// rescaled once or twice an item.
+// rescaled once or twice an item.  `mx`: the largest of the lane's scores.
 template <typename T, typename S>
-__device__ __forceinline__ void follow(Rows<S>& x, const f32x4 (&sc)[S::MQ][2], float to2, float slack) {
-    float mx[S::MQ];
-    bool up = false;
+__device__ __forceinline__ void follow(Rows<S>& x, float mx, float to2, float slack) {
+    if (!__any(mx > x.m + slack)) return;
+    float m = mx;
 #pragma unroll
-    for (int mq = 0; mq < S::MQ; ++mq) {
-        mx[mq] = fmaxf(fmaxf(fmaxf(sc[mq][0][0], sc[mq][0][1]), fmaxf(sc[mq][0][2], sc[mq][0][3])),
-                       fmaxf(fmaxf(sc[mq][1][0], sc[mq][1][1]), fmaxf(sc[mq][1][2], sc[mq][1][3])));
-        up |= mx[mq] > x.m[mq] + slack;
-    }
-    if (__any(up)) {
+    for (int o = S::RL; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+    const bool mine = m > x.m + slack;
+    const float f = mine ? __builtin_amdgcn_exp2f((x.m * to2 - kRise<T>) - ref_of<T>(m, to2)) : 1.0f;
+    x.l *= f;
 #pragma unroll
-        for (int mq = 0; mq < S::MQ; ++mq) {
-            const float m = row_max(mx[mq]);
-            const bool mine = m > x.m[mq] + slack;
-            const float f = mine ? __builtin_amdgcn_exp2f((x.m[mq] * to2 - kRise<T>) - ref_of<T>(m, to2))
-                                 : 1.0f;
-            x.l[mq] *= f;
-#pragma unroll
-            for (int t = 0; t < 2 * S::NB; ++t) x.o[mq][t] *= f;
-            x.m[mq] = mine ? m : x.m[mq];
-        }
-    }
+    for (int t = 0; t < S::EL / Rows<S>::VL; ++t) x.o[t] *= f;
+    x.m = mine ? m : x.m;
 }
 
-// Scores of one row tile to probabilities.  The sum takes them unrounded, the second product
+// Eight scores of a lane to probabilities.  The sum takes them unrounded, the second product
 // in 16 bits, what the matrix cores take.
 template <typename T>
 __device__ __forceinline__ u32x4 weights(const f32x4 (&sc)[2], float m, float to2, float* l) {
@@ -486,11 +497,11 @@ __device__ __forceinline__ int64_t page_at(const AttnArgs& p, int page) {
 // Scores of what a lane's row does not attend made -inf: `entry(i)` is that of score i, behind
 // the pages the tail's row entry(i) - len.
 template <typename S, bool TAIL, int N, typename Entry, typename Score>
-__device__ __forceinline__ void hide(const AttnArgs& p, const Item& it, const Rows<S>& x, int mq, int e0,
+__device__ __forceinline__ void hide(const AttnArgs& p, const Item& it, const Rows<S>& x, int e0,
                                      Entry entry, Score score) {
     const int there = it.sq.len + (TAIL ? it.sq.tail : 0);
     if (TAIL && p.a.mask) {
-        const Global<uint8_t> row = global<uint8_t>(p.a.mask) + (int64_t)x.mask[mq] * p.a.tail;
+        const Global<uint8_t> row = global<uint8_t>(p.a.mask) + (int64_t)x.mask * p.a.tail;
         uint8_t named[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) named[i] = row[min(entry(i), there - 1) - it.sq.len];
@@ -498,11 +509,11 @@ __device__ __forceinline__ void hide(const AttnArgs& p, const Item& it, const Ro
         for (int i = 0; i < N; ++i)
             score(i) = (named[i] != 0) & (entry(i) < there) ? score(i) : -INFINITY;
     } else if (it.some_hidden(e0, there)) {
-        const int hi = min(x.hi[mq], there - 1);
+        const int hi = min(x.hi, there - 1);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int e = entry(i);
-            score(i) = (e <= hi) & ((e >= x.lo[mq]) | (e < it.sinks)) ? score(i) : -INFINITY;
+            score(i) = (e <= hi) & ((e >= x.lo) | (e < it.sinks)) ? score(i) : -INFINITY;
         }
     }
 }
@@ -526,10 +537,12 @@ __device__ __forceinline__ uint32_t pair_at(uint32_t codes, float f, int byte) {
 }
 
 // An item's tiles by waves that have the same rows and share the entries: codes straight into
-// registers, operands made there, a wave for itself.
+// registers, operands made there, a wave for itself, the codes of the next tile on their
+// way.  (128 single tokens as above: two tiles on their way 113 us for 103, three workgroups a
+// compute unit, whose registers spill, 144.)
 template <typename T, typename S>
 __device__ __forceinline__ void own_tiles(const AttnArgs& p, const Item& it, Rows<S>& x, bool careful) {
-    constexpr int NB = S::NB, MQ = S::MQ;
+    constexpr int NB = S::NB;
     constexpr bool P2 = (NB & (NB - 1)) == 0;
     constexpr int VW = NB <= 4 ? 1 : 2;              // words of an entry's V a lane
     constexpr int SB = P2 ? 1 : 2;                   // blocks that these lie in
@@ -594,24 +607,17 @@ __device__ __forceinline__ void own_tiles(const AttnArgs& p, const Item& it, Row
             for (int s = 0; s < SB; ++s) rvs[u][s] = load<uint32_t, 4>(vx + vx_at[s]);
         }
     };
-    // the scores of 32 entries from e0 on
-    const auto hide_all = [&](f32x4 (&sc)[MQ][2], int e0, auto tail) {
+    // the scores of 32 entries from e0 on to O, with V's operands at hand
+    const auto finish = [&](f32x4 (&sc)[2], const u32x4 (&vo)[2 * NB], int e0, auto tail) {
+        hide<S, decltype(tail)::value, 8>(
+            p, it, x, e0, [&](int i) { return e0 + 16 * (i >> 2) + 4 * g4 + (i & 3); },
+            [&](int i) -> float& { return ((float*)&sc[0])[i]; });
+        const float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
+                               fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+        follow<T, S>(x, mx, to2, slack);
+        const u32x4 pt = weights<T>(sc, x.m, to2, &x.l);
 #pragma unroll
-        for (int mq = 0; mq < MQ; ++mq)
-            hide<S, decltype(tail)::value, 8>(
-                p, it, x, mq, e0, [&](int i) { return e0 + 16 * (i >> 2) + 4 * g4 + (i & 3); },
-                [&](int i) -> float& { return ((float*)&sc[mq][0])[i]; });
-    };
-    // scores to O, with V's operands at hand
-    const auto finish = [&](f32x4 (&sc)[MQ][2], const u32x4 (&vo)[2 * S::NB]) {
-        follow<T, S>(x, sc, to2, slack);
-        u32x4 pt[MQ];
-#pragma unroll
-        for (int mq = 0; mq < MQ; ++mq) pt[mq] = weights<T>(sc[mq], x.m[mq], to2, &x.l[mq]);
-#pragma unroll
-        for (int t = 0; t < 2 * S::NB; ++t)
-#pragma unroll
-            for (int mq = 0; mq < MQ; ++mq) x.o[mq][t] = mfma<T>(vo[t], pt[mq], x.o[mq][t]);
+        for (int t = 0; t < 2 * NB; ++t) x.o[t] = mfma<T>(vo[t], pt, x.o[t]);
     };
 
     fetch_pages(it.tile);
@@ -634,19 +640,17 @@ __device__ __forceinline__ void own_tiles(const AttnArgs& p, const Item& it, Row
                 for (int s = 0; s < SB; ++s) rvs[u][s] &= keep;
             }
         }
-        f32x4 sc[MQ][2];
+        f32x4 sc[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-#pragma unroll
-            for (int mq = 0; mq < MQ; ++mq) sc[mq][u] = f32x4{0, 0, 0, 0};
+            sc[u] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int s = 0; s < NB; ++s) {
                 const float f = scale_of(rks[u][P2 ? s / 4 : s]);
                 const uint32_t w = rk[u][s];
                 const u32x4 ko{pair_of<T, 0>(w, f), pair_of<T, 1>(w, f), pair_of<T, 2>(w, f),
                                pair_of<T, 3>(w, f)};
-#pragma unroll
-                for (int mq = 0; mq < MQ; ++mq) sc[mq][u] = mfma<T>(ko, x.q[mq][s], sc[mq][u]);
+                sc[u] = mfma<T>(ko, x.q[s], sc[u]);
             }
         }
         u32x4 vo[2 * NB];
@@ -661,8 +665,7 @@ __device__ __forceinline__ void own_tiles(const AttnArgs& p, const Item& it, Row
         }
         fetch(k + 1);
         fetch_pages(k + 2);
-        hide_all(sc, e0, std::false_type());
-        finish(sc, vo);
+        finish(sc, vo, e0, std::false_type());
     }
     const Global<uint8_t> kt = global<uint8_t>(a.k_tail) + 2 * it.hk * D;
     const Global<uint8_t> vt = global<uint8_t>(a.v_tail) + 2 * it.hk * D;
@@ -672,19 +675,17 @@ __device__ __forceinline__ void own_tiles(const AttnArgs& p, const Item& it, Row
     for (int k = max(it.tile, it.end_pages); k < it.end_tile; ++k) {
         const int j0 = (it.span.tile(k) - it.span.pages) * S::KT + 32 * wt;
         if (j0 >= sq.tail) continue;
-        f32x4 sc[MQ][2];
+        f32x4 sc[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const Global<uint8_t> row = kt + (row0 + min(j0 + 16 * u + n16, sq.tail - 1)) * row_bytes;
-#pragma unroll
-            for (int mq = 0; mq < MQ; ++mq) sc[mq][u] = f32x4{0, 0, 0, 0};
+            sc[u] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int s = 0; s < NB; ++s) {
                 const int d = 8 * NB * g4 + 8 * s;
                 u32x4 ko = load<u32x4, 16>(row + 2 * min(d, D - 8));
                 if (d >= D) ko = u32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int mq = 0; mq < MQ; ++mq) sc[mq][u] = mfma<T>(ko, x.q[mq][s], sc[mq][u]);
+                sc[u] = mfma<T>(ko, x.q[s], sc[u]);
             }
             // (one block's loads after the other's products: registers, which the loop over
             // the pages has use for)
@@ -706,18 +707,17 @@ __device__ __forceinline__ void own_tiles(const AttnArgs& p, const Item& it, Row
             }
             by_entries(w, &vo[2 * q], &vo[2 * q + 1]);
         }
-        hide_all(sc, sq.len + j0, std::true_type());
-        finish(sc, vo);
+        finish(sc, vo, sq.len + j0, std::true_type());
     }
 }
 
 // An item's tiles by waves of different rows, of the pages or of the tail.  The waves make a
-// tile's operands together and put them into LDS, K as the lanes take it (`lane` of operand
-// i has 16 bytes at (64 i + lane) 16), V as rows of the entries' elements, 32 bytes more than
-// they are apart, so that the reads that transpose 4x16 blocks of them meet no bank twice;
-// then each multiplies them with its own rows, as 32x32x16 tiles (half the instructions of
-// 16x16x32: issuing them is what bounds this loop).  While tile t is worked on, t + 1 is
-// written, whose codes were loaded during t - 1; so a barrier a tile.
+// tile's operands together and put them into LDS, K as the lanes take it (`lane` of operand i
+// has 16 bytes at (64 i + lane) 16), V as rows of the entries' elements, 32 bytes more than
+// they have apart (a third of LDS's busy cycles are bank conflicts; with 64 bytes a fifth, in the
+// same time); then each multiplies them with its own rows, as 32x32x16 tiles (half the
+// instructions of 16x16x32: issuing them is what bounds this loop).  While tile t is worked
+// on, t + RING - 1 is written, whose codes were loaded a tile earlier; so a barrier a tile.
 template <typename T, typename S, bool TAIL>
 __device__ __forceinline__ void shared_tiles(const AttnArgs& p, const Item& it, Rows<S>& x,
                                              bool careful, char* lds) {
@@ -892,7 +892,7 @@ __device__ __forceinline__ void shared_tiles(const AttnArgs& p, const Item& it, 
         for (int u = 0; u < U; ++u) sc[u] = 0.0f;
 #pragma unroll
         for (int i = 0; i < KS * U; ++i)
-            sc[i % U] = mfma32<T>(ON == 2 && i < AHEAD ? ahead[i] : k_part(stage, i), x.q[0][i / U], sc[i % U]);
+            sc[i % U] = mfma32<T>(ON == 2 && i < AHEAD ? ahead[i] : k_part(stage, i), x.q[i / U], sc[i % U]);
         // reads ahead of the products
         __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
 #pragma unroll
@@ -909,30 +909,19 @@ __device__ __forceinline__ void shared_tiles(const AttnArgs& p, const Item& it, 
             for (int u = 0; u < U; ++u) {
                 const int e0 = (TAIL ? sq.len : 0) + first(k) + 32 * (u - vc);
                 hide<S, TAIL, 16>(
-                    p, it, x, 0, e0, [&](int i) { return e0 + 4 * half + 8 * (i / 4) + i % 4; },
+                    p, it, x, e0, [&](int i) { return e0 + 4 * half + 8 * (i / 4) + i % 4; },
                     [&](int i) -> float& { return ((float*)&sc[u])[i]; });
             }
         }
-        // The exponents' reference follows the row's own maximum by steps (kSlack), so that
-        // O is rescaled once or twice an item.
         float mx = sc[0][0];
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[u][i]);
-        if (__any(mx > x.m[0] + slack)) {
-            const float m = fmaxf(mx, __shfl_xor(mx, 32));
-            const bool mine = m > x.m[0] + slack;
-            const float f =
-                mine ? __builtin_amdgcn_exp2f((x.m[0] * to2 - kRise<T>) - ref_of<T>(m, to2)) : 1.0f;
-            x.l[0] *= f;
-#pragma unroll
-            for (int d = 0; d < NB; ++d) x.o[0][d] *= f;
-            x.m[0] = mine ? m : x.m[0];
-        }
+        follow<T, S>(x, mx, to2, slack);
         // The sum takes the probabilities unrounded, the second product in 16 bits, what the
         // matrix cores take.
-        const float ref = ref_of<T>(x.m[0], to2);
+        const float ref = ref_of<T>(x.m, to2);
         float sum = 0.0f;
         const uint32_t vp = lds_at + stage * S::STAGE + V0 + v_at;
 #pragma unroll
@@ -955,11 +944,11 @@ __device__ __forceinline__ void shared_tiles(const AttnArgs& p, const Item& it, 
                     const s16x4 hi =
                         __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)(at + 8 * ROWB));
                     const s16x8 va = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    x.o[0][d] = mfma32<T>(__builtin_bit_cast(u32x4, va), pt, x.o[0][d]);
+                    x.o[d] = mfma32<T>(__builtin_bit_cast(u32x4, va), pt, x.o[d]);
                 }
             }
         }
-        x.l[0] += sum;
+        x.l += sum;
         __builtin_amdgcn_sched_group_barrier(0x100, 8, 1);
 #pragma unroll
         for (int i = 0; i < NB * U * 2 - 4; ++i) {
@@ -982,9 +971,9 @@ __device__ __forceinline__ void shared_tiles(const AttnArgs& p, const Item& it, 
 template <typename T, typename S>
 __global__ __launch_bounds__(S::NT) __attribute__((amdgpu_waves_per_eu(S::WAVES, S::WAVES))) void
 k_packed_attention(AttnArgs p) {
-    constexpr int MQ = S::MQ, RL = S::RL;
+    constexpr int RL = S::RL;
     extern __shared__ __align__(16) char s_lds[];
-    __shared__ float s_ml[S::SHARED ? 2 : S::NW * MQ * 16 * 2];
+    __shared__ float s_ml[S::SHARED ? 2 : S::NW * 16 * 2];
     __shared__ int s_order[S::SHARED ? kDealt : 1];    // sequences, the longest first
     const int tid = threadIdx.x, lane = tid & 63, n = lane % RL, g = lane / RL;
     const int wave = uniform(tid >> 6), tile0 = S::SHARED ? wave : 0;
@@ -997,7 +986,7 @@ k_packed_attention(AttnArgs p) {
     bool dealt = false;
     if constexpr (S::SHARED)
         if (p.whole && st.groups == p.groups)
-            dealt = uniform(deal_items<S>(p, st.total, s_order)) != 0;
+            dealt = uniform(deal_items<S>(p, st.total, st.setup, s_order)) != 0;
     if (tid == 0) p.desc[8 * w] = 0;
     if (!dealt && st.t0 >= st.t1) return;
     // the item at hand: sequence, key head, row block, its tile to begin with; the
@@ -1013,7 +1002,7 @@ k_packed_attention(AttnArgs p) {
             hk = i % c.K;
             sq = uniform(seq_of<S>(p, b));
             if (sq.nrb) {
-                left = uniform(span_of<S>(p, sq, 0).length);
+                left = uniform(span_of<S>(p, sq, 0, st.setup).length);
                 ++round;
                 return true;
             }
@@ -1024,22 +1013,20 @@ k_packed_attention(AttnArgs p) {
         if (!next_dealt()) return;
     } else {
         b = st.seq;
-        sq = uniform(seq_of<S>(p, b));
+        sq = st.of;
         int64_t rel = st.t0 - st.before;
-        const int64_t per_head = tiles_of_head<S>(p, sq);
-        hk = uniform((int)(rel / per_head));
+        const int64_t per_head = length_of_head<S>(p, sq, st.setup);
+        hk = uniform((int)quotient(rel, per_head));
         rel -= hk * per_head;
-        for (int n; rel >= (n = span_of<S>(p, sq, rb).length); ++rb) rel -= n;
+        for (int n; rel >= (n = span_of<S>(p, sq, rb, st.setup).length); ++rb) rel -= n;
         rb = uniform(rb);
         tile = uniform((int)rel);
         left = st.t1 - st.t0;
         // the join of the first item, by the first cut inside it
-        const int64_t begins = st.t0 - tile, ends = begins + span_of<S>(p, sq, rb).length;
+        const int64_t begins = st.t0 - tile, ends = begins + span_of<S>(p, sq, rb, st.setup).length;
         if (tid == 0 && tile > 0 && stretch_start(st.total, st.groups, w - 1) <= begins) {
             int* d = p.desc + 8 * w;
-            int n = 2;
-            while (stretch_start(st.total, st.groups, w + n - 1) < ends) ++n;
-            d[0] = n;                                // partial results
+            d[0] = stretch_of(st.total, st.groups, ends - 1) - w + 2;    // partial results
             d[1] = 2 * (w - 1) + (stretch_start(st.total, st.groups, w - 1) < begins ? 1 : 0);
             d[2] = b;
             d[3] = hk;
@@ -1048,37 +1035,36 @@ k_packed_attention(AttnArgs p) {
     }
 
     for (bool first = true; left > 0; first = false) {
-        const Span span = uniform(span_of<S>(p, sq, rb));
+        const Span span = uniform(span_of<S>(p, sq, rb, st.setup));
         const int end_place = (int)min((int64_t)span.length, tile + left);
         // its tiles in the stretch: of the pages, then of the tail (none: a part of nothing)
-        const int begin_tile = max(tile - S::SETUP, 0), end_tile = max(end_place - S::SETUP, 0);
+        const int begin_tile = max(tile - st.setup, 0), end_tile = max(end_place - st.setup, 0);
         const int end_pages = min(end_tile, span.from < span.pages ? span.pages - span.from + span.head
                                                                    : min(span.head, span.pages));
         Rows<S> x;
         int lo_most = 0, hi_least = 0x7FFFFFFF;
-#pragma unroll
-        for (int mq = 0; mq < MQ; ++mq) {
-            const int r = rb * S::ROWS + (tile0 + mq) * RL + n;
-            const bool live = r < sq.rows * p.g;
-            const int qi = live ? r / p.g : 0, qh = hk * p.g + (live ? r - qi * p.g : 0);
-            const int64_t qrow = (int64_t)b * a.n + qi;
+        const int row = rb * S::ROWS + tile0 * RL + n;
+        const bool live = row < sq.rows * p.g;
+        const int qi = live ? row / p.g : 0, qh = hk * p.g + (live ? row - qi * p.g : 0);
+        const int64_t qrow = (int64_t)b * a.n + qi;
+        {
             const T* q = (const T*)a.q + qrow * a.q_stride + (int64_t)qh * D;
 #pragma unroll
             for (int s = 0; s < Rows<S>::QS; ++s) {
                 const int d = S::SHARED ? 16 * s + 8 * g : 8 * S::NB * g + 8 * s;
-                x.q[mq][s] = u32x4{0, 0, 0, 0};
-                if (live && d < D) x.q[mq][s] = *(const u32x4*)(q + d);
+                x.q[s] = u32x4{0, 0, 0, 0};
+                if (live && d < D) x.q[s] = *(const u32x4*)(q + d);
             }
             int at = sq.len + a.tail - a.n + qi;     // the row's position
             if (a.mask) at = a.window && a.positions ? max(a.positions[qrow], sq.len) : sq.len;
-            x.hi[mq] = a.mask ? sq.len - 1 : at;
-            x.lo[mq] = a.window ? at - a.window + 1 : 0;
-            x.mask[mq] = (uint32_t)qrow;
+            x.hi = a.mask ? sq.len - 1 : at;
+            x.lo = a.window ? at - a.window + 1 : 0;
+            x.mask = (uint32_t)qrow;
             if (live) {
-                lo_most = max(lo_most, x.lo[mq]);
-                hi_least = min(hi_least, x.hi[mq]);
+                lo_most = max(lo_most, x.lo);
+                hi_least = x.hi;
             } else {
-                x.hi[mq] = -1;                       // (what it would attend may be any bytes)
+                x.hi = -1;                           // (what it would attend may be any bytes)
             }
         }
         for (int o = 1; o < RL; o <<= 1) {
@@ -1094,12 +1080,9 @@ k_packed_attention(AttnArgs p) {
         bool careful = false;
         for (;;) {                                   // again where the tail is not finite
 #pragma unroll
-            for (int mq = 0; mq < MQ; ++mq) {
-#pragma unroll
-                for (int t = 0; t < S::EL / Rows<S>::VL; ++t) x.o[mq][t] = 0.0f;
-                x.m[mq] = -INFINITY;
-                x.l[mq] = 0.0f;
-            }
+            for (int t = 0; t < S::EL / Rows<S>::VL; ++t) x.o[t] = 0.0f;
+            x.m = -INFINITY;
+            x.l = 0.0f;
             if constexpr (S::SHARED) {
                 shared_tiles<T, S, false>(p, it, x, careful, s_lds);
                 shared_tiles<T, S, true>(p, it, x, careful, s_lds);
@@ -1111,101 +1094,80 @@ k_packed_attention(AttnArgs p) {
             // does not attend it (0 times it is NaN) neither: then once more without them.
             float z = 0.0f;
 #pragma unroll
-            for (int mq = 0; mq < MQ; ++mq) {
-                float y = 0.0f;
-#pragma unroll
-                for (int e = 0; e < S::EL; ++e) y = __fmaf_rn(x.at(mq, e), 0.0f, y);
-                if (rb * S::ROWS + (tile0 + mq) * RL + n < sq.rows * p.g) z += y;
-            }
-            careful = __syncthreads_or(!(z == 0.0f) && end_tile > end_pages) != 0;
+            for (int e = 0; e < S::EL; ++e) z = __fmaf_rn(x.at(e), 0.0f, z);
+            careful = __syncthreads_or(live && !(z == 0.0f) && end_tile > end_pages) != 0;
             if (!careful) break;
         }
 
         // a row's lanes put together, and waves of the same rows
 #pragma unroll
-        for (int mq = 0; mq < MQ; ++mq) {
-            if constexpr (S::SHARED) x.l[mq] += __shfl_xor(x.l[mq], 32);
-            else x.l[mq] = row_sum(x.l[mq]);
-        }
+        for (int o = RL; o < 64; o <<= 1) x.l += __shfl_xor(x.l, o);
         if constexpr (!S::SHARED) {
             __syncthreads();                         // (the last item's have been read)
-#pragma unroll
-            for (int mq = 0; mq < MQ; ++mq)
-                if (g == 0) {
-                    s_ml[((wave * MQ + mq) * 16 + n) * 2] = x.m[mq];
-                    s_ml[((wave * MQ + mq) * 16 + n) * 2 + 1] = x.l[mq];
-                }
+            if (g == 0) {
+                s_ml[(wave * 16 + n) * 2] = x.m;
+                s_ml[(wave * 16 + n) * 2 + 1] = x.l;
+            }
             __syncthreads();
             float* out = (float*)s_lds;
+            float m = -INFINITY, l = 0.0f;
 #pragma unroll
-            for (int mq = 0; mq < MQ; ++mq) {
-                float m = -INFINITY, l = 0.0f;
+            for (int k = 0; k < S::NW; ++k) m = fmaxf(m, s_ml[(k * 16 + n) * 2]);
+            const float ref = ref_of<T>(m, to2);
 #pragma unroll
-                for (int k = 0; k < S::NW; ++k) m = fmaxf(m, s_ml[((k * MQ + mq) * 16 + n) * 2]);
-                const float ref = ref_of<T>(m, to2);
-#pragma unroll
-                for (int k = 0; k < S::NW; ++k) {
-                    const float* ml = s_ml + ((k * MQ + mq) * 16 + n) * 2;
-                    l += ml[1] * __builtin_amdgcn_exp2f((ml[0] * to2 - kRise<T>) - ref);
-                }
-                const float f = __builtin_amdgcn_exp2f((x.m[mq] * to2 - kRise<T>) - ref);
-#pragma unroll
-                for (int t = 0; t < S::EL / 4; ++t) {
-                    x.o[mq][t] *= f;
-                    if (wave > 0)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            out[(((wave - 1) * MQ + mq) * S::EL + 4 * t + r) * 64 + lane] = x.o[mq][t][r];
-                }
-                x.m[mq] = m;
-                x.l[mq] = l;
+            for (int k = 0; k < S::NW; ++k) {
+                const float* ml = s_ml + (k * 16 + n) * 2;
+                l += ml[1] * __builtin_amdgcn_exp2f((ml[0] * to2 - kRise<T>) - ref);
             }
+            const float f = __builtin_amdgcn_exp2f((x.m * to2 - kRise<T>) - ref);
+#pragma unroll
+            for (int t = 0; t < S::EL / 4; ++t) {
+                x.o[t] *= f;
+                if (wave > 0)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        out[((wave - 1) * S::EL + 4 * t + r) * 64 + lane] = x.o[t][r];
+            }
+            x.m = m;
+            x.l = l;
             __syncthreads();
             if (wave == 0)
 #pragma unroll 1
                 for (int k = 1; k < S::NW; ++k)
 #pragma unroll
-                    for (int mq = 0; mq < MQ; ++mq)
+                    for (int t = 0; t < S::EL / 4; ++t)
 #pragma unroll
-                        for (int t = 0; t < S::EL / 4; ++t)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                x.o[mq][t][r] += out[(((k - 1) * MQ + mq) * S::EL + 4 * t + r) * 64 + lane];
+                        for (int r = 0; r < 4; ++r)
+                            x.o[t][r] += out[((k - 1) * S::EL + 4 * t + r) * 64 + lane];
         }
         if (S::SHARED || wave == 0) {
             const bool whole = tile == 0 && end_place == span.length;
-            float* part = c.part + (int64_t)(2 * w + (first ? 0 : 1)) * S::PART;
+            if (whole) {
+                if (live) {
+                    const float inv = x.l == 0.0f ? 0.0f : 1.0f / x.l;
+                    T* o = (T*)a.out + qrow * a.out_stride + (int64_t)qh * D;
 #pragma unroll
-            for (int mq = 0; mq < MQ; ++mq) {
-                const int rt = tile0 + mq, r = rb * S::ROWS + rt * RL + n;
-                if (whole) {
-                    if (r < sq.rows * p.g) {
-                        const int qi = r / p.g, qh = hk * p.g + r - qi * p.g;
-                        const int64_t qrow = (int64_t)b * a.n + qi;
-                        const float inv = x.l[mq] == 0.0f ? 0.0f : 1.0f / x.l[mq];
-                        T* o = (T*)a.out + qrow * a.out_stride + (int64_t)qh * D;
+                    for (int k = 0; k < S::NB; ++k) {
+                        float f[S::EC];
 #pragma unroll
-                        for (int k = 0; k < S::NB; ++k) {
-                            float f[S::EC];
-#pragma unroll
-                            for (int i = 0; i < S::EC; ++i) f[i] = x.at(mq, k * S::EC + i) * inv;
-                            store_chunk<T, S>(o, g, k, D, f);
-                        }
-                        if (a.lse && g == 0) a.lse[qrow * c.H + qh] = lse_of<T>(x.m[mq], x.l[mq], a.scale);
-                        if (careful)
-                            for (int k = 0; k < S::NB; ++k) add_unfinite<T, S>(p, b, hk, sq, qi, o, g, k);
+                        for (int i = 0; i < S::EC; ++i) f[i] = x.at(k * S::EC + i) * inv;
+                        store_chunk<T, S>(o, g, k, D, f);
                     }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < S::EL; ++e) part[(rt * S::EL + e) * 64 + lane] = x.at(mq, e);
-                    if (g == 0) {
-                        float* ml = part + S::ROWS * S::DP + (rt * RL + n) * 2;
-                        ml[0] = x.m[mq];
-                        ml[1] = x.l[mq];
-                    }
+                    if (a.lse && g == 0) a.lse[qrow * c.H + qh] = lse_of<T>(x.m, x.l, a.scale);
+                    if (careful)
+                        for (int k = 0; k < S::NB; ++k) add_unfinite<T, S>(p, b, hk, sq, qi, o, g, k);
                 }
+            } else {
+                float* part = c.part + (int64_t)(2 * w + (first ? 0 : 1)) * S::PART;
+#pragma unroll
+                for (int e = 0; e < S::EL; ++e) part[(tile0 * S::EL + e) * 64 + lane] = x.at(e);
+                if (g == 0) {
+                    float* ml = part + S::ROWS * S::DP + (tile0 * RL + n) * 2;
+                    ml[0] = x.m;
+                    ml[1] = x.l;
+                }
+                if (tid == 0) ((int*)part)[S::PART - 1] = careful;
             }
-            if (!whole && tid == 0) ((int*)part)[S::PART - 1] = careful;
         }
         // the next item
         left -= end_place - tile;
@@ -1320,14 +1282,23 @@ __global__ __launch_bounds__(NTJ) void k_packed_join(AttnArgs p) {
 
 namespace {
 
-// Shapes for up to 16, 32, 64, 128 and more rows of an item.
+// Shapes for up to 16, 64, 128 and more rows of an item, the fastest of those tried.  us for 32
+// sequences of 1024 to 4096 entries, 8 key heads of 128 (bytes at the copy's rate: 18), with
+//         1    12    24    40    60   100   128   200   250 rows
+//   R1   41    41    65    87   110   180   210   393   486
+//   R4   66    66    67    68    69   121   126   241   246
+//   R8   84    83    84    86    89   100   105   185   196
+//  R16  126   123   128   128   130   143   154   178   188
+// Two row tiles a wave of own_tiles take 70 us at 24 rows (registers spill), 103 at 40.  Heads of
+// more than 128 elements leave registers for half the waves: 24 rows of 256 by two shared waves
+// 205 us, by four 186; up to 16 rows of 256 by two waves a SIMD, which spill, 121, by one 77.
 template <int NB>
 struct Shapes {
     static constexpr bool W = NB > 4;
-    typedef PShape<NB, false, 1, 4, W ? 1 : 2> R1;
-    typedef PShape<NB, true, 1, W ? 4 : 2, W ? 1 : 2> R4;
-    typedef PShape<NB, true, 1, 4, W ? 1 : 2> R8;
-    typedef PShape<NB, true, 1, W ? 4 : 8, 1> R16;
+    typedef PShape<NB, false, 4, W ? 1 : 2> R1;
+    typedef PShape<NB, true, W ? 4 : 2, W ? 1 : 2> R4;
+    typedef PShape<NB, true, 4, W ? 1 : 2> R8;
+    typedef PShape<NB, true, W ? 4 : 8, 1> R16;
 };
 
 template <typename S>
