@@ -551,8 +551,9 @@ typedef struct rheo_packed_attention_args {
  * i, its position (so with tail 0 the rows are the pages' last entries).  With a window
  * it does not attend entries at or below its position - window, but for the first `sinks`;
  * a mask says all about the tail, the window being about the pages alone then.  A page
- * none of whose entries some row attends is not read.  Infinite and NaN values of the
- * tail act on the rows that attend them alone. */
+ * none of whose entries some row attends is not read (with a mask: none of whose entries
+ * a row at position lens[b] would attend).  Infinite and NaN values of the tail act on
+ * the rows that attend them alone. */
 int rheo_packed_attention(rheo_cache* cache, const rheo_packed_attention_args* args, void* stream);
 
 typedef struct rheo_packed_commit_args {

@@ -691,6 +691,8 @@ class PackedCache(Cache):
         plan's; sequences that it did not serve are left out."""
         B, n = self.B, q.shape[1]
         p_q, q_row = self._rows(q, n, self.H, "q")
+        if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):
+            _refuse("window and sinks must be in [0, 2^31)")
         if (k_tail is None) != (v_tail is None):
             _refuse("k_tail and v_tail: both or none")
         tail = tail_row = 0

@@ -20,8 +20,8 @@
 // of 128, fp16, 358 MB) 98 us where a copy's rate would take 72; what is over is the line, the
 // items' beginnings one after another, and some workgroups' slower memory.  Up to 256 rows,
 // issuing instructions: 64 trees of 244 rows over 1000 to 4096 entries (8 key heads, 0.27 GB,
-// 176 GFLOP) 212 us, 830 TFLOP/s, where a large product's rate would take 152.  A SIMD's two
-// waves have 2160 cycles of products a tile of 64 entries and 560 vector operations, each 4.6
+// 176 GFLOP) 216 us, 815 TFLOP/s, where a large product's rate would take 152.  A SIMD's two
+// waves have 2160 cycles of products a tile of 64 entries and 490 vector operations, each 4.6
 // cycles (measured beside products: 6 + 4.6 n a product of 16.9); one wave's chain alone is
 // some 3150 cycles, and the tile takes 4900.  No gain came from one of the two waves half a
 // tile later (211 to 237 us), from their priorities, from loads two tiles ahead, or from a
@@ -115,6 +115,13 @@ struct Span {
     __device__ __forceinline__ int tile(int k) const { return k < head ? k : k - head + from; }
 };
 
+// The first entry in the window of a row at position `at`.  Positions and windows may be as
+// large as 2^31 - 1, and a row without entries stands before the first: neither wraps
+// (entries are fewer than 2^30 + 2^24, and sums of one with a tile stay in 32 bits).
+__device__ __forceinline__ int window_begin(int at, int window) {
+    return min(max(at, 0) - window + 1, 0x7FFF0000);
+}
+
 template <typename S>
 __device__ __forceinline__ Span span_of(const AttnArgs& p, const Seq& s, int rb, int setup = 0) {
     const rheo_packed_attention_args& a = p.a;
@@ -127,7 +134,7 @@ __device__ __forceinline__ Span span_of(const AttnArgs& p, const Seq& s, int rb,
         const int last = min(((rb + 1) * S::ROWS - 1) / p.g, s.rows - 1);
         x.hi = min(x.hi, s.len + a.tail - a.n + last);
     }
-    if (a.window) x.lo = max(first - a.window + 1, 0);
+    if (a.window) x.lo = max(window_begin(first, a.window), 0);
     x.pages = (s.len + S::KT - 1) / S::KT;
     const auto tile_of = [&](int e) {
         return e < s.len ? e / S::KT : x.pages + (e - s.len) / S::KT;
@@ -1058,7 +1065,7 @@ k_packed_attention(AttnArgs p) {
             int at = sq.len + a.tail - a.n + qi;     // the row's position
             if (a.mask) at = a.window && a.positions ? max(a.positions[qrow], sq.len) : sq.len;
             x.hi = a.mask ? sq.len - 1 : at;
-            x.lo = a.window ? at - a.window + 1 : 0;
+            x.lo = a.window ? window_begin(at, a.window) : 0;
             x.mask = (uint32_t)qrow;
             if (live) {
                 lo_most = max(lo_most, x.lo);
