@@ -514,13 +514,13 @@ __device__ __forceinline__ void hide(const AttnArgs& p, const Item& it, const Ro
         for (int i = 0; i < N; ++i) named[i] = row[min(entry(i), there - 1) - it.sq.len];
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            score(i) = (named[i] != 0) & (entry(i) < there) ? score(i) : -INFINITY;
+            score(i) = ((named[i] != 0) & (entry(i) < there)) ? score(i) : -INFINITY;
     } else if (it.some_hidden(e0, there)) {
         const int hi = min(x.hi, there - 1);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int e = entry(i);
-            score(i) = (e <= hi) & ((e >= x.lo) | (e < it.sinks)) ? score(i) : -INFINITY;
+            score(i) = ((e <= hi) & ((e >= x.lo) | (e < it.sinks))) ? score(i) : -INFINITY;
         }
     }
 }

@@ -42,3 +42,46 @@ def test_windows_that_32_bits_do_not_hold_are_refused(binding):  # noqa: F811
         with pytest.raises(binding.RheoError):
             case.call(**more)
     case.c.close()
+
+
+def test_calls_without_rows(binding):  # noqa: F811
+    """Nothing is read or written, whatever the addresses."""
+    case = Case(binding, BF16, [20, 5], 2, 2, 1, 64, 16)
+    c, (kp, vp) = case.c, case.pool
+    was = kp.clone(), vp.clone()
+    none = torch.empty((2, 0, 1, 64), dtype=BF16, device="cuda")
+    slots = torch.empty((2, 0), dtype=torch.int64, device="cuda")
+    c.append(none, none, slots, kp, vp)
+    assert [x.shape for x in c.read(slots, kp, vp)] == [none.shape] * 2
+    assert torch.equal(kp, was[0]) and torch.equal(vp, was[1])
+    case.q = torch.empty((2, 0, 2, 64), dtype=BF16)
+    out, lse = case.call(lse=True)
+    assert out.shape == (2, 0, 2, 64) and lse.shape == (2, 0, 2)
+    assert c.device_error() == 0
+    c.close()
+
+
+@pytest.mark.parametrize("n,H", [(1, 4), (61, 4)])
+def test_two_caches_at_once_on_two_streams(binding, n, H):  # noqa: F811
+    """Each handle has partial results of its own."""
+    cases = [Case(binding, BF16, [900 + 50 * s, 1300], n, H, 1, 128, 16, seed=s) for s in (1, 2)]
+    alone = [case.call() for case in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    args = []
+    for case in cases:
+        args.append(dict(k_tail=case.k_tail.cuda(), v_tail=case.v_tail.cuda()))
+    q = [case.q.cuda() for case in cases]
+    table = [torch.tensor(case.table, dtype=torch.int32, device="cuda") for case in cases]
+    lens = [torch.tensor(case.lens, dtype=torch.int32, device="cuda") for case in cases]
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(20):
+        for i, case in enumerate(cases):
+            outs[i].append(case.c.attention(q[i], *case.pool, table[i], lens[i], stream=streams[i],
+                                            **args[i]))
+    torch.cuda.synchronize()
+    for want, got in zip(alone, outs):
+        assert all(torch.equal(want, x) for x in got)
+    for case in cases:
+        case.c.close()
