@@ -20,14 +20,14 @@
 // of 128, fp16, 358 MB) 98 us where a copy's rate would take 72; what is over is the line, the
 // items' beginnings one after another, and some workgroups' slower memory.  Up to 256 rows,
 // issuing instructions: 64 trees of 244 rows over 1000 to 4096 entries (8 key heads, 0.27 GB,
-// 176 GFLOP) 216 us, 815 TFLOP/s, where a large product's rate would take 152.  A SIMD's two
-// waves have 2160 cycles of products a tile of 64 entries and 490 vector operations, each 4.6
-// cycles (measured beside products: 6 + 4.6 n a product of 16.9); one wave's chain alone is
-// some 3150 cycles, and the tile takes 4900.  No gain came from one of the two waves half a
-// tile later (211 to 237 us), from their priorities, from loads two tiles ahead, or from a
-// chunk's scores one chunk ahead (registers spill: 1624 us).  Scores by the matrix cores' own
-// 4-bit operands (K as it is, q in two parts of 8 bits) are no faster, and off by 2^-16 of the
-// sum of |q k|.
+// 176 GFLOP) 205 us, 860 TFLOP/s (216 on some boxes), where a large product's would take 152.
+// A SIMD's two waves have 2160 cycles of products a tile of 64 entries and 490 vector
+// operations, each 4.6 cycles (measured beside products: 6 + 4.6 n a product of 16.9); one
+// wave's chain alone is some 3150 cycles, and the tile takes 4900.  No gain came from one of
+// the two waves half a tile later (211 to 237 us), from their priorities, from loads two tiles
+// ahead, or from a chunk's scores one chunk ahead (registers spill: 1624 us).  Scores by the
+// matrix cores' own 4-bit operands (K as it is, q in two parts of 8 bits) are no faster, and
+// off by 2^-16 of the sum of |q k|.
 #pragma once
 
 #include <type_traits>
@@ -466,6 +466,7 @@ struct Item {
     int tile, end_pages, end_tile;           // the stretch's tiles of it: the pages', the tail's
     int lo_most, hi_least, sinks;            // entries that all rows of the wave attend:
                                              // lo_most to hi_least
+    bool idle;                               // the wave has no rows
     // Whether some row attends entry e of the pages; one of the 16 from e on (others are not
     // read); whether no row attends one of the 32 from e on; whether one of the wave's rows
     // does not attend one of these.
@@ -889,6 +890,20 @@ __device__ __forceinline__ void shared_tiles(const AttnArgs& p, const Item& it, 
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) ahead[i] = k_part(0, i);
     int stage = 0;                                   // of tile k
+    // A wave without rows makes its part of the operands only.  (32 sequences of 0 to 488 rows
+    // over some 20000 entries: 574 us to 524.)
+    if (it.idle) {
+#pragma unroll 1
+        for (int k = begin; k < end; ++k) {
+            stage = stage + 1 == S::RING ? 0 : stage + 1;
+            put(k + ON, ON == 1 ? stage : stage + 1 == S::RING ? 0 : stage + 1);
+            fetch(k + ON + 1);
+            fetch_pages(k + ON + 2);
+            barrier();
+        }
+        if (outside) atomicOr(c.err, CE_PAGE);
+        return;
+    }
 #pragma unroll 1
     for (int k = begin; k < end; ++k) {
         const int next = stage + 1 == S::RING ? 0 : stage + 1;
@@ -1083,7 +1098,8 @@ k_packed_attention(AttnArgs p) {
         const int sinks = a.window ? a.sinks : 0;
 
         const Item it{uniform(b),         uniform(hk),       uniform(rb), sq,       span, uniform(begin_tile),
-                      uniform(end_pages), uniform(end_tile), lo_most,     hi_least, sinks};
+                      uniform(end_pages), uniform(end_tile), lo_most,     hi_least, sinks,
+                      !uniform(__any(live))};
         bool careful = false;
         for (;;) {                                   // again where the tail is not finite
 #pragma unroll
