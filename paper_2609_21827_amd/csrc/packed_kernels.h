@@ -473,8 +473,10 @@ struct Item {
     __device__ __forceinline__ bool attended(int e) const {
         return e < sq.len && e <= span.hi && (e >= span.lo || e < sinks);
     }
+    // (the window may begin behind the pages' end: the last of the 16 that is there decides)
     __device__ __forceinline__ bool wanted(int e) const {
-        return e < sq.len && e <= span.hi && (e + 15 >= span.lo || e < sinks);
+        const int last = min(e + 15, min(sq.len - 1, span.hi));
+        return e <= last && (last >= span.lo || e < sinks);
     }
     __device__ __forceinline__ bool some_idle(int e) const {
         return !(e + 31 < sq.len && e + 31 <= span.hi && (e >= span.lo || e + 31 < sinks));
