@@ -3,7 +3,7 @@
 
 namespace rheo {
 
-template struct PackedHeads<1>;
-template struct PackedHeads<8>;
+PackedHeads packed_heads_1() { return packed_heads<1>(); }
+PackedHeads packed_heads_8() { return packed_heads<8>(); }
 
 }  // namespace rheo

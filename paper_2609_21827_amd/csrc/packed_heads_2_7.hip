@@ -3,7 +3,7 @@
 
 namespace rheo {
 
-template struct PackedHeads<2>;
-template struct PackedHeads<7>;
+PackedHeads packed_heads_2() { return packed_heads<2>(); }
+PackedHeads packed_heads_7() { return packed_heads<7>(); }
 
 }  // namespace rheo

@@ -3,7 +3,7 @@
 
 namespace rheo {
 
-template struct PackedHeads<3>;
-template struct PackedHeads<6>;
+PackedHeads packed_heads_3() { return packed_heads<3>(); }
+PackedHeads packed_heads_6() { return packed_heads<6>(); }
 
 }  // namespace rheo

@@ -3,7 +3,7 @@
 
 namespace rheo {
 
-template struct PackedHeads<4>;
-template struct PackedHeads<5>;
+PackedHeads packed_heads_4() { return packed_heads<4>(); }
+PackedHeads packed_heads_5() { return packed_heads<5>(); }
 
 }  // namespace rheo

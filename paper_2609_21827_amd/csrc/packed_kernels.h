@@ -33,6 +33,7 @@
 #include <type_traits>
 
 #include "packed_format.h"
+#include "packed_heads.h"
 #include "softmax_ref.h"
 
 namespace rheo {
@@ -1380,26 +1381,28 @@ hipError_t prepare_rows() {
     return e == hipSuccess ? allow_lds<T, typename H::R16>() : e;
 }
 
-}  // namespace
-
-// The launches for heads of NB blocks of 32 elements; compiled one or two NB to a source.
 template <int NB>
-struct PackedHeads {
-    static hipError_t prepare(int dtype) {
-        return dtype == RHEO_BF16 ? prepare_rows<__bf16, NB>() : prepare_rows<_Float16, NB>();
-    }
-    // floats of partial results, without the descriptions of the joins
-    static size_t workspace(int units) { return rheo::workspace<NB>(units); }
-    static hipError_t launch(const CacheDev& c, const PackedDev& d, const rheo_packed_attention_args& a,
-                             int* desc, hipStream_t s) {
-        AttnArgs p{};
-        p.c = c;
-        p.p = d;
-        p.a = a;
-        p.g = c.H / c.K;
-        p.desc = desc;
-        return c.dtype == RHEO_BF16 ? start_rows<__bf16, NB>(p, s) : start_rows<_Float16, NB>(p, s);
-    }
-};
+hipError_t prepare(int dtype) {
+    return dtype == RHEO_BF16 ? prepare_rows<__bf16, NB>() : prepare_rows<_Float16, NB>();
+}
+
+template <int NB>
+hipError_t launch(const CacheDev& c, const PackedDev& d, const rheo_packed_attention_args& a, int* desc,
+                  hipStream_t s) {
+    AttnArgs p{};
+    p.c = c;
+    p.p = d;
+    p.a = a;
+    p.g = c.H / c.K;
+    p.desc = desc;
+    return c.dtype == RHEO_BF16 ? start_rows<__bf16, NB>(p, s) : start_rows<_Float16, NB>(p, s);
+}
+
+template <int NB>
+PackedHeads packed_heads() {
+    return PackedHeads{prepare<NB>, workspace<NB>, launch<NB>};
+}
+
+}  // namespace
 
 }  // namespace rheo
