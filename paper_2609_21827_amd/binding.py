@@ -605,6 +605,18 @@ class PackedCache(Cache):
         """Not of 4-bit pages, which take finished rows (``append``)."""
         _refuse("rows are written into the tail, by a Cache whose pages are the tail's rows")
 
+    def _apart(self, s, layers):
+        """Bytes between pages and between layers of pages of these strides; those of
+        dimensions of one element say nothing."""
+        page = self.K * self.page_bytes
+        if s[-1] != 1 or (self.K > 1 and s[-2] != self.page_bytes):
+            _refuse("a page's bytes must be dense")
+        row = s[-3] if self.pages > 1 else page
+        layer = s[0] if layers is not None and layers > 1 else self.pages * row
+        if row < page or layer < (self.pages - 1) * row + page:
+            _refuse("pages must not overlap")
+        return row, layer
+
     def _packed(self, k, v, layers=None):
         """PackedPages of one layer, or of `layers`."""
         shape = self._head_shape if layers is None else (layers,) + self._head_shape
@@ -613,15 +625,9 @@ class PackedCache(Cache):
                     or t.get_device() != self._index:
                 _refuse(f"{name} must be {torch.uint8} {shape} on {self.device}")
         s = k.stride()
-        if v.stride() != s:
+        row, layer = self._apart(s, layers)
+        if v.stride() != s and self._apart(v.stride(), layers) != (row, layer):
             _refuse("k_pages and v_pages must have the same strides")
-        page = self.K * self.page_bytes
-        if s[-1] != 1 or (self.K > 1 and s[-2] != self.page_bytes):
-            _refuse("a page's bytes must be dense")
-        row = s[-3] if self.pages > 1 else page
-        layer = s[0] if layers is not None and layers > 1 else self.pages * row
-        if row < page or layer < (self.pages - 1) * row + page:
-            _refuse("pages must not overlap")
         return PackedPages(k.data_ptr(), v.data_ptr(), row, layer)
 
     def _layers_rows(self, t, n, layers, name):
