@@ -494,7 +494,7 @@ typedef struct rheo_packed_pages {
                                     page_stride                                       */
 } rheo_packed_pages;
 
-/* Bytes of one head's page, page_size * nb * 17. */
+/* Bytes of one head's page, page_size * nb * 17; 0 for sizes that no handle of such pages has. */
 int32_t rheo_packed_page_bytes(int32_t head_dim, int32_t page_size);
 
 typedef struct rheo_packed_rows {

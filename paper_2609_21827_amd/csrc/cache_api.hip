@@ -334,6 +334,9 @@ int rheo_cache_commit_served(rheo_cache* c, int32_t n, int32_t depth, const int3
 }
 
 int32_t rheo_packed_page_bytes(int32_t head_dim, int32_t page_size) {
+    if (head_dim < 8 || head_dim > 256 || head_dim % 8 || page_size < 16 || page_size > 4096 ||
+        (page_size & (page_size - 1)))
+        return 0;
     return page_size * ((head_dim + 31) / 32) * 17;
 }
 
