@@ -429,7 +429,10 @@ typedef struct rheo_attention_args {
  * accumulators; the probabilities enter the second product in cfg.dtype.  A row
  * that attends nothing gives 0 and lse -inf.  Rows i >= count[b] are left as
  * they were.  What a row does not attend has no effect on it, whatever it
- * holds; keys that it does attend are finite (else its output may be NaN). */
+ * holds; keys that it does attend are finite, scaled scores at most 2^22 in
+ * magnitude and, with RHEO_BF16, the magnitudes of its finite values at most
+ * 2^118 in sum (else its output may be infinite or NaN: sums are held in fp32,
+ * with weights up to 2^8). */
 int rheo_tree_attention(rheo_cache* cache, const rheo_attention_args* args, void* stream);
 
 /* Keeps the accepted path of a verified tree: with parent and token [B][n] as
@@ -548,12 +551,12 @@ typedef struct rheo_packed_attention_args {
 
 /* rheo_tree_attention over the pages (entries 0 to lens[b] - 1) and the tail behind them
  * (entries lens[b] + j).  Without a mask, row i attends up to entry lens[b] + tail - n +
- * i, its position (so with tail 0 the rows are the pages' last entries).  With a window
- * it does not attend entries at or below its position - window, but for the first `sinks`;
- * a mask says all about the tail, the window being about the pages alone then.  A page
- * none of whose entries some row attends is not read (with a mask: none of whose entries
- * a row at position lens[b] would attend).  Infinite and NaN values of the tail act on
- * the rows that attend them alone. */
+ * i, its position (so with tail 0 the n rows are the pages' last n entries, whatever
+ * count[b]).  With a window it does not attend entries at or below its position - window,
+ * but for the first `sinks`; a mask says all about the tail, the window being about the
+ * pages alone then.  A page none of whose entries some row attends is not read (with a
+ * mask: none of whose entries a row at position lens[b] would attend).  Infinite and NaN
+ * values of the tail act on the rows that attend them alone. */
 int rheo_packed_attention(rheo_cache* cache, const rheo_packed_attention_args* args, void* stream);
 
 typedef struct rheo_packed_commit_args {

@@ -690,11 +690,11 @@ class PackedCache(Cache):
                   status=None, stream=None):
         """Attention of q [B, n, heads, head_dim] over each sequence's pages (``lens`` entries)
         and the tail behind them that mask [B, n, tail] uint8 names; without a mask, causal,
-        the rows being the last n entries.  window: entries that a row reaches back (0: all),
-        but for the first ``sinks``; with a mask, from ``positions`` [B, n] int32 (the
-        plan's; by default the pages' end).  Returns out, or (out, lse) where lse is True or a
-        tensor [B, n, heads] float32.  scale: 1 / sqrt(head_dim) by default.  status: the
-        plan's; sequences that it did not serve are left out."""
+        row i being entry lens + tail - n + i (whatever ``count``).  window: entries that a
+        row reaches back (0: all), but for the first ``sinks``; with a mask, from ``positions``
+        [B, n] int32 (the plan's; by default the pages' end).  Returns out, or (out, lse) where
+        lse is True or a tensor [B, n, heads] float32.  scale: 1 / sqrt(head_dim) by default.
+        status: the plan's; sequences that it did not serve are left out."""
         B, n = self.B, q.shape[1]
         p_q, q_row = self._rows(q, n, self.H, "q")
         if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):
