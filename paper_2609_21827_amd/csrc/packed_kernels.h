@@ -17,10 +17,10 @@
 // from the first row's window on.
 //
 // What bounds it.  Few rows, memory: 128 single tokens over 2000 to 8191 entries (4 key heads
-// of 128, fp16, 358 MB) 98 us where a copy's rate would take 72; what is over is the line, the
+// of 128, fp16, 358 MB) 93 us where a copy's rate would take 72; what is over is the line, the
 // items' beginnings one after another, and some workgroups' slower memory.  Up to 256 rows,
 // issuing instructions: 64 trees of 244 rows over 1000 to 4096 entries (8 key heads, 0.27 GB,
-// 176 GFLOP) 205 us, 860 TFLOP/s (216 on some boxes), where a large product's would take 152.
+// 176 GFLOP) 210 to 215 us by box, 818 to 838 TFLOP/s, where a large product's would take 152.
 // A SIMD's two waves have 2160 cycles of products a tile of 64 entries and 490 vector
 // operations, each 4.6 cycles (measured beside products: 6 + 4.6 n a product of 16.9); one
 // wave's chain alone is some 3150 cycles, and the tile takes 4900.  No gain came from one of
@@ -390,7 +390,10 @@ __device__ __forceinline__ void follow(Rows<S>& x, float mx, float to2, float sl
 }
 
 // Eight scores of a lane to probabilities.  The sum takes them unrounded, the second product
-// in 16 bits, what the matrix cores take.
+// in 16 bits, what the matrix cores take.  That is a choice, rheo_tree_attention's: the rounding
+// is off by nearly as much again as the output's (trees over 4096 entries, bf16: 2.3e-3 of the
+// norm against 64 bits, 1.7e-3 by the output's alone), and a second product with what it left
+// over would lengthen a loop that is bound by issuing instructions.
 template <typename T>
 __device__ __forceinline__ u32x4 weights(const f32x4 (&sc)[2], float m, float to2, float* l) {
     const float ref = ref_of<T>(m, to2);
@@ -1308,16 +1311,18 @@ __global__ __launch_bounds__(NTJ) void k_packed_join(AttnArgs p) {
 
 namespace {
 
-// Shapes for up to 16, 64, 128 and more rows of an item, the fastest of those tried.  us for 32
-// sequences of 1024 to 4096 entries, 8 key heads of 128 (bytes at the copy's rate: 18), with
+// Shapes for up to 16, 64, 128 and more rows of an item.  us a call for 32 sequences of 1024 to
+// 4096 entries, 8 key heads of 128 (bytes at the copy's rate: 18), with
 //         1    12    24    40    60   100   128   200   250 rows
-//   R1   41    41    65    87   110   180   210   393   486
-//   R4   66    66    67    68    69   121   126   241   246
-//   R8   84    83    84    86    89   100   105   185   196
-//  R16  126   123   128   128   130   143   154   178   188
-// Two row tiles a wave of own_tiles take 70 us at 24 rows (registers spill), 103 at 40.  Heads of
-// more than 128 elements leave registers for half the waves: 24 rows of 256 by two shared waves
-// 205 us, by four 186; up to 16 rows of 256 by two waves a SIMD, which spill, 121, by one 77.
+//   R1   39    39    59    79    97   161   181   287   362
+//   R4   63    61    62    64    64   103   103   178   192
+//   R8   66    65    66    74    74    83    85   129   145
+//  R16   90    90    90    92    94    98    99   118   136
+// (R1, which takes such rows 16 at a time, would do for a few more than 16.)  Two row tiles a wave
+// of own_tiles take 70 us at 24 rows (registers spill), 103 at 40.  Heads of more than 128
+// elements leave registers for half the waves: 24 rows of 256 by two shared waves 174 us, by four
+// 144 (bytes: 36; R1 127, but 177 for 149 at 40 rows); up to 16 rows of 256 by two waves a SIMD,
+// which spill, 118, by one 73.
 template <int NB>
 struct Shapes {
     static constexpr bool W = NB > 4;

@@ -62,8 +62,9 @@ __device__ __forceinline__ bool store_part(const CacheDev& c, const PackedDev& p
 // the exponent.  A workgroup takes ROWS rows at a time, head after head, so that what
 // it writes of a head's page (or reads) is 16 entries next to each other where their slots are:
 // 1 KB of codes instead of 64 bytes here and there, which the chip's eight L2 would each
-// write a part of.  Bound by memory: 12064 rows of 40 heads of 80, 203 MB, 59 us into pages
-// (79 row by row) and 39 out of them (59).
+// write a part of.  Bound by memory: 12064 rows of 40 heads of 80, 204 MB, 58 us into pages (79
+// row by row; a copy's rate 41; 180 MB fetched for the rows' 154, 52 written for 49), and 37 out of
+// them again, in part from the memory's cache (59).
 
 template <typename T, int NB, int ROWS, bool READ>
 __global__ __launch_bounds__(NTP) void k_packed_rows(CacheDev c, PackedDev p, rheo_packed_rows r,
@@ -145,9 +146,9 @@ __global__ __launch_bounds__(NTP) void k_packed_rows(CacheDev c, PackedDev p, rh
 // Every block of a sequence walks the accepted path for itself, then rounds its share of
 // the layers' rows into the pages, a part of all the path's rows a thread.  Rows and pages are
 // different memory, so the order is free.  The sequence's last block writes the length, which
-// may be lens itself.  Bound by memory, and by writes of less than its lines: 128 sequences, 32
-// layers, 5 entries on average (100 MB) 35 us; one sequence 5, the walk's latency.  (The
-// path's rows of a head by neighbouring threads: 39 to 51 us.)
+// may be lens itself.  Bound by memory, after the walk: 128 sequences, 32 layers, 5 entries on
+// average (108 MB; 86 fetched, 28 written for 23) 34 us (a copy's rate 22); one sequence 5, the
+// walk's latency.  (The path's rows of a head by neighbouring threads: 39 to 51 us.)
 template <typename T>
 __global__ __launch_bounds__(NTP) void k_packed_commit(CacheDev c, PackedDev p,
                                                        rheo_packed_commit_args a, int split) {
@@ -243,7 +244,7 @@ hipError_t by_blocks(int nb, F f) {
 template <typename T, bool READ>
 hipError_t start_rows(const CacheDev& c, const PackedDev& p, const rheo_packed_rows& r, hipStream_t s) {
     return by_blocks(p.nb, [&](auto nb) {
-        // a sequence's few rows are next to no others: one at a time (one row of 8 heads 2.8 us,
+        // a sequence's few rows are next to no others: one at a time (one row of 8 heads 2.7 us,
         // as one of 16 5.4)
         const int rows = r.n < 8 ? 1 : 16;
         const int64_t groups = ((int64_t)c.B * r.n + rows - 1) / rows;
